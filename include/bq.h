@@ -217,6 +217,66 @@ bq_status bq_residual_split(const float *e, int64_t rows, int32_t cols, void *pi
 bq_status bq_quantiser_grad(const void *v, const void *vq, float *g, const float *factor, const bq_quant *quant,
                             const bq_rows *rows, void *stream);
 
+/* ---- quantised linear layers ------------------------------------------------------------------- */
+
+/* INT8 codes of rows of any width, one scale per row (the activation side of a layer in 8-bit integers; rows that
+ * bq_butterfly_fwd has rotated, or any others).  The quantiser is the one of bq_butterfly_fwd_quant with bits = 8 and the row
+ * as its group: amax = max|v|; s = amax / 127; if scale_dtype is BQ_F16, s = half(s), saturating at 65504; inv = 1 / s;
+ * q = clip(rint(v * inv), -128, 127).  A scale below 2^-126 counts as 0 (scale and codes 0).  A row that holds an infinity or a
+ * NaN gets the scale NaN and codes 0: a product with it is NaN.
+ *   x     : [rows][ld_x] of dtype (bq_dtype), cols used elements per row, ld_x >= cols (elements)
+ *   codes : [rows][ld_codes] bytes, ld_codes >= cols; bytes behind the columns are left as they were
+ *   scales: [rows] of scale_dtype (BQ_F32 or BQ_F16)
+ * 0 <= rows < 2^31, 1 <= cols <= 2^24, rows * max(ld_x, ld_codes) <= 2^44. */
+bq_status bq_rows_quant8(const void *x, int64_t rows, int32_t cols, int64_t ld_x, int32_t dtype, int8_t *codes,
+                         int64_t ld_codes, void *scales, int32_t scale_dtype, void *stream);
+
+/* A linear layer on codes.  Codes are two's-complement fields of 8, 4 or 2 bits, the lowest channel in the lowest bits of a
+ * byte, as bq_rows_quant8 and bq_butterfly_fwd_quant (group = n) write them. */
+typedef struct {
+    int64_t rows;        /* tokens, 0 <= rows < 2^31                                                    */
+    int32_t inputs;      /* K: 1 .. 131071 (the sums are exact in 32 bits)                              */
+    int32_t outputs;     /* N: 1 .. 2^24; 1 .. 131071 for the gradient                                  */
+    int32_t experts;     /* weight matrices, 1 .. 4096; 1 for bq_linear_fwd and bq_linear_bwd            */
+    int32_t xbits;       /* 8 or 4 (not used by the gradient)                                           */
+    int32_t wbits;       /* 8, 4 or 2                                                                   */
+    int32_t dtype;       /* bq_dtype of y and bias, or of dy and dx                                     */
+    int32_t scale_dtype; /* BQ_F32 or BQ_F16, of xscale and wscale                                      */
+    int32_t reserved;
+    int64_t ld_x;        /* row stride of x in bytes (>= ceil(K xbits / 8)); of dx in elements (>= K)    */
+    int64_t ld_w;        /* row stride of w in bytes (>= ceil(K wbits / 8))                             */
+    int64_t ld_y;        /* row stride of y or dy in elements (>= N)                                    */
+} bq_linear;
+
+/* y[t][o] = xscale[t] * wscale[o] * sum_k x[t][k] w[o][k] + bias[o]   (the layer's product Q(Bx) . Q(WB^T) of the
+ * reconstruction loss, with one scale per token and one per output channel).  The sum is exact in 32-bit integers; it is
+ * converted to float32, multiplied with the scales and added to the bias there, and rounded once to dtype.
+ *   x: [rows][ld_x], w: [N][ld_w], xscale: [rows], wscale: [N], bias: [N] of dtype or NULL, y: [rows][ld_y].
+ * y must not overlap the inputs.  Pointers of x and w aligned to 16 bytes with ld_x, ld_w and the rows' bytes K bits / 8
+ * multiples of 16 are what the fast kernels take; anything else is computed by a slower one, with the same results. */
+bq_status bq_linear_fwd(const void *x, const void *xscale, const void *w, const void *wscale, const void *bias, void *y,
+                        const bq_linear *desc, void *stream);
+
+/* The gradient with respect to the dequantised rows:  dx[t][k] = sum_o dy[t][o] wscale[o] w[o][k]   (the weights are codes and
+ * stay as they are; with a straight-through round dx is the gradient of the rows that were quantised).  dy * wscale is taken
+ * as a fixed-point number relative to the row's largest |dy * wscale|, of 16 bits for 16-bit rows and of 24 for float32: it is
+ * off by at most 2^-15.9 or 2^-21.6 of that largest one, and the sums are exact.  Rows whose entries are all below
+ * 2^-120 give 0; a row with an infinity or a NaN in dy * wscale gives NaN throughout.
+ *   dy: [rows][ld_y], dx: [rows][ld_x], both of dtype; workspace: at least the queried size, 256-byte aligned, its contents
+ *   on entry are ignored.  dx must not overlap dy. */
+size_t bq_linear_bwd_workspace_bytes(const bq_linear *desc); /* 0 if the descriptor is invalid */
+bq_status bq_linear_bwd(const void *dy, const void *w, const void *wscale, void *dx, void *workspace,
+                        size_t workspace_bytes, const bq_linear *desc, void *stream);
+
+/* The same for rows sorted by expert: rows offsets[e] .. offsets[e + 1] - 1 are multiplied with expert e's weights.
+ *   offsets: [experts + 1] int32 on the device, non-decreasing, between 0 and rows (values outside are taken as the nearest
+ *   one inside).  An expert may have no rows.  Rows before offsets[0] and from offsets[experts] on are left as they were.
+ *   w: [experts][N][ld_w], wscale: [experts][N], bias: [experts][N] or NULL. */
+bq_status bq_linear_grouped_fwd(const void *x, const void *xscale, const void *w, const void *wscale, const void *bias,
+                                const int32_t *offsets, void *y, const bq_linear *desc, void *stream);
+bq_status bq_linear_grouped_bwd(const void *dy, const void *w, const void *wscale, const int32_t *offsets, void *dx,
+                                void *workspace, size_t workspace_bytes, const bq_linear *desc, void *stream);
+
 /* ---- measurement helpers (not part of the method) ------------------------------------------- */
 
 /* dst[0, bytes) = src[0, bytes): a plain streaming copy (16 bytes per lane), the reference for what the memory

@@ -28,6 +28,8 @@ EXPORTS = ["bq_plan_bytes", "bq_plan_build", "bq_butterfly_fwd", "bq_butterfly_i
            "bq_butterfly_fwd_fakequant", "bq_hadamard_fwd", "bq_cayley_build", "bq_kron_fwd", "bq_kron_inv",
            "bq_butterfly_bwd_workspace_bytes", "bq_butterfly_bwd", "bq_butterfly_bwd_static",
            "bq_butterfly_bwd_static_max_bytes", "bq_residual_scratch_bytes", "bq_residual_split", "bq_quantiser_grad",
+           "bq_rows_quant8", "bq_linear_fwd", "bq_linear_bwd_workspace_bytes", "bq_linear_bwd", "bq_linear_grouped_fwd",
+           "bq_linear_grouped_bwd",
            "bq_probe_copy", "bq_probe_read", "bq_probe_read_sink_bytes",
            "bq_probe_fma", "bq_probe_fma_out_floats",
            "bq_status_string", "bq_last_error",
@@ -43,6 +45,12 @@ class bq_rows(ctypes.Structure):
 class bq_quant(ctypes.Structure):
     _fields_ = [("bits", ctypes.c_int32), ("group", ctypes.c_int32), ("scale_dtype", ctypes.c_int32),
                 ("reserved", ctypes.c_int32)]
+
+
+class bq_linear(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("inputs", ctypes.c_int32), ("outputs", ctypes.c_int32), ("experts", ctypes.c_int32),
+                ("xbits", ctypes.c_int32), ("wbits", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale_dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("ld_x", ctypes.c_int64), ("ld_w", ctypes.c_int64), ("ld_y", ctypes.c_int64)]
 
 
 class BqError(RuntimeError):
@@ -87,6 +95,16 @@ def lib() -> ctypes.CDLL:
         L.bq_residual_split.restype = ctypes.c_int
         L.bq_quantiser_grad.argtypes = [vp, vp, vp, vp, ctypes.POINTER(bq_quant), ctypes.POINTER(bq_rows), vp]
         L.bq_quantiser_grad.restype = ctypes.c_int
+        i32, i64, lin = ctypes.c_int32, ctypes.c_int64, ctypes.POINTER(bq_linear)
+        L.bq_rows_quant8.argtypes = [vp, i64, i32, i64, i32, vp, i64, vp, i32, vp]
+        L.bq_linear_fwd.argtypes = [vp] * 6 + [lin, vp]
+        L.bq_linear_grouped_fwd.argtypes = [vp] * 7 + [lin, vp]
+        L.bq_linear_bwd.argtypes = [vp] * 5 + [sz, lin, vp]
+        L.bq_linear_grouped_bwd.argtypes = [vp] * 6 + [sz, lin, vp]
+        for f in (L.bq_rows_quant8, L.bq_linear_fwd, L.bq_linear_grouped_fwd, L.bq_linear_bwd, L.bq_linear_grouped_bwd):
+            f.restype = ctypes.c_int
+        L.bq_linear_bwd_workspace_bytes.argtypes = [lin]
+        L.bq_linear_bwd_workspace_bytes.restype = sz
         L.bq_butterfly_bwd_workspace_bytes.argtypes = [ctypes.POINTER(bq_rows)]
         L.bq_butterfly_bwd_workspace_bytes.restype = sz
         L.bq_butterfly_bwd.argtypes = [vp, vp, vp, vp, vp, vp, sz, ctypes.POINTER(bq_rows), vp]
@@ -119,6 +137,10 @@ _CALLS = None
 _KINDS = {"bq_plan_build": "piipus", "bq_butterfly_fwd": "ppprs", "bq_butterfly_inv": "ppprs", "bq_butterfly_fwd_quant": "ppppqrs",
           "bq_butterfly_fwd_fakequant": "ppppqrs", "bq_kron_fwd": "pppiprs", "bq_kron_inv": "pppiprs", "bq_butterfly_bwd": "ppppppurs"}
 
+# the same for the calls of the quantised linear layers, whose descriptor is a bq_linear ("l")
+_LINEAR_KINDS = {"bq_rows_quant8": "puiuipupis", "bq_linear_fwd": "ppppppls", "bq_linear_grouped_fwd": "pppppppls",
+                 "bq_linear_bwd": "pppppuls", "bq_linear_grouped_bwd": "ppppppuls"}
+
 
 def _general_call(name: str, kinds: str):
     """An entry point through its ctypes prototype, with the arguments a Caller takes."""
@@ -126,7 +148,7 @@ def _general_call(name: str, kinds: str):
 
     def call(*args):
         try:
-            return fn(*[_ptr(a) if k == "p" else ctypes.byref(a) if k in "rq" else a for k, a in zip(kinds, args)])
+            return fn(*[_ptr(a) if k == "p" else ctypes.byref(a) if k in "rql" else a for k, a in zip(kinds, args)])
         except ctypes.ArgumentError as e:
             raise TypeError(str(e)) from None
 
@@ -134,7 +156,7 @@ def _general_call(name: str, kinds: str):
 
 
 class _Calls:
-    """One callable per entry point of _KINDS, without the "bq_" in front: a Caller, or its ctypes prototype where `path` does not exist."""
+    """One callable per entry point of _KINDS and _LINEAR_KINDS, without the "bq_" in front: a Caller, or its ctypes prototype where `path` does not exist."""
 
     def __init__(self, path: str = CALL_PATH):
         L = lib()
@@ -143,11 +165,12 @@ class _Calls:
             loader = importlib.machinery.ExtensionFileLoader("bqcall", path)
             module = importlib.util.module_from_spec(importlib.util.spec_from_loader("bqcall", loader))
             loader.exec_module(module)
-        for name, kinds in _KINDS.items():
-            call = _general_call(name, kinds)
-            if module:
-                call = module.Caller(ctypes.cast(getattr(L, name), ctypes.c_void_p).value, kinds, bq_rows, bq_quant, call)
-            setattr(self, name[3:], call)
+        for table, descriptor in ((_KINDS, bq_rows), (_LINEAR_KINDS, bq_linear)):
+            for name, kinds in table.items():
+                call = _general_call(name, kinds)
+                if module:
+                    call = module.Caller(ctypes.cast(getattr(L, name), ctypes.c_void_p).value, kinds, descriptor, bq_quant, call)
+                setattr(self, name[3:], call)
 
 
 def _calls() -> _Calls:
@@ -319,6 +342,100 @@ def bq_butterfly_bwd_static_max_bytes() -> int:
     return int(lib().bq_butterfly_bwd_static_max_bytes())
 
 
+_here = None
+
+
+def _require_tensors(who: str, tensors) -> None:
+    """What the library cannot see in a bare pointer.  tensors: (name, tensor or None, its types, the elements it has to have, whether
+    it has to be contiguous).  Every one has to be on the current device, whose stream the call goes to."""
+    global _here
+    if _here is None:
+        import torch
+
+        torch.cuda.init()
+        _here = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    device = _here()
+    for name, t, types, count, dense in tensors:
+        if t is None:  # the library's own check
+            continue
+        if t.get_device() != device:
+            raise BqError(2, f"{who}: {name} is on {t.device}, the current device is cuda:{device}")
+        if t.dtype not in types:
+            raise BqError(3, f"{who}: {name} is {t.dtype}")
+        if t.numel() < count or (dense and not t.is_contiguous()):
+            raise BqError(2, f"{who}: {name} must have at least {count} elements{' and be contiguous' if dense else ''}")
+
+
+_TYPES = None
+
+
+def _torch_types(code: int):
+    """The torch type of a bq_dtype, as a tuple; -1: codes."""
+    global _TYPES
+    if _TYPES is None:
+        import torch
+
+        _TYPES = {BQ_F32: (torch.float32,), BQ_F16: (torch.float16,), BQ_BF16: (torch.bfloat16,), -1: (torch.int8, torch.uint8),
+                  -2: (torch.int32,), -3: (torch.uint8,)}
+    return _TYPES.get(code, ())
+
+
+def bq_rows_quant8(x, codes, scales, stream=None) -> None:
+    """x: [rows, cols] of any row type, codes: int8 [rows, cols], both with a contiguous last dimension; scales: [rows], float32 or
+    float16."""
+    rows, cols = x.shape
+    ld_x, ld_codes = (x.stride(0), codes.stride(0)) if rows > 1 else (cols, cols)
+    _require(x.stride(1) == codes.stride(1) == 1 or cols == 1 or rows == 0, 2, "bq_rows_quant8: the last dimension must be contiguous")
+    _require(codes.shape == x.shape, 2, "bq_rows_quant8: codes and x differ in shape")
+    _require_tensors("bq_rows_quant8", (("x", x, _torch_types(BQ_F32) + _torch_types(BQ_F16) + _torch_types(BQ_BF16), 0, False),
+                                        ("codes", codes, _torch_types(-1), 0, False),
+                                        ("scales", scales, _torch_types(BQ_F32) + _torch_types(BQ_F16), rows, True)))
+    _check((_CALLS or _calls()).rows_quant8(x, rows, cols, ld_x, _dtype_code(x), codes, ld_codes, scales, _dtype_code(scales), _stream_ptr(stream)))
+
+
+def bq_linear_bwd_workspace_bytes(desc: bq_linear) -> int:
+    return int(lib().bq_linear_bwd_workspace_bytes(ctypes.byref(desc)))
+
+
+def _linear_tensors(d: bq_linear, x, xscale, w, wscale, bias, y):
+    per_channel, scales, values = d.experts * d.outputs, _torch_types(d.scale_dtype), _torch_types(d.dtype)
+    return (("x", x, _torch_types(-1), (d.inputs * d.xbits + 7) // 8 * d.rows, False), ("xscale", xscale, scales, d.rows, True),
+            ("w", w, _torch_types(-1), (d.inputs * d.wbits + 7) // 8 * per_channel, False), ("wscale", wscale, scales, per_channel, True),
+            ("bias", bias, values, per_channel, True), ("y", y, values, d.rows * d.outputs, False))
+
+
+def _linear_bwd_tensors(d: bq_linear, dy, w, wscale, dx, workspace):
+    per_channel, values = d.experts * d.outputs, _torch_types(d.dtype)
+    return (("dy", dy, values, d.rows * d.outputs, False), ("w", w, _torch_types(-1), (d.inputs * d.wbits + 7) // 8 * per_channel, False),
+            ("wscale", wscale, _torch_types(d.scale_dtype), per_channel, True), ("dx", dx, values, d.rows * d.inputs, False),
+            ("workspace", workspace, _torch_types(-3), 0, True))
+
+
+def bq_linear_fwd(x, xscale, w, wscale, bias, y, desc: bq_linear, stream=None) -> None:
+    """desc: make_linear(x, w, wscale, y, ...); bias may be None."""
+    _require_tensors("bq_linear_fwd", _linear_tensors(desc, x, xscale, w, wscale, bias, y))
+    _check((_CALLS or _calls()).linear_fwd(x, xscale, w, wscale, bias, y, desc, _stream_ptr(stream)))
+
+
+def bq_linear_grouped_fwd(x, xscale, w, wscale, bias, offsets, y, desc: bq_linear, stream=None) -> None:
+    """Rows sorted by expert; offsets: int32 [experts + 1] on the device."""
+    _require_tensors("bq_linear_grouped_fwd", _linear_tensors(desc, x, xscale, w, wscale, bias, y) +
+                     (("offsets", offsets, _torch_types(-2), desc.experts + 1, True),))
+    _check((_CALLS or _calls()).linear_grouped_fwd(x, xscale, w, wscale, bias, offsets, y, desc, _stream_ptr(stream)))
+
+
+def bq_linear_bwd(dy, w, wscale, dx, workspace, desc: bq_linear, stream=None) -> None:
+    """desc: make_linear_bwd(dy, w, wscale, dx, ...); workspace: uint8, at least bq_linear_bwd_workspace_bytes(desc)."""
+    _require_tensors("bq_linear_bwd", _linear_bwd_tensors(desc, dy, w, wscale, dx, workspace))
+    _check((_CALLS or _calls()).linear_bwd(dy, w, wscale, dx, workspace, workspace.numel(), desc, _stream_ptr(stream)))
+
+
+def bq_linear_grouped_bwd(dy, w, wscale, offsets, dx, workspace, desc: bq_linear, stream=None) -> None:
+    _require_tensors("bq_linear_grouped_bwd", _linear_bwd_tensors(desc, dy, w, wscale, dx, workspace) +
+                     (("offsets", offsets, _torch_types(-2), desc.experts + 1, True),))
+    _check((_CALLS or _calls()).linear_grouped_bwd(dy, w, wscale, offsets, dx, workspace, workspace.numel(), desc, _stream_ptr(stream)))
+
+
 def bq_probe_copy(src, dst, nbytes: int, stream=None) -> None:
     _check(lib().bq_probe_copy(_ptr(src), _ptr(dst), nbytes, _stream_ptr(stream)))
 
@@ -374,3 +491,51 @@ def make_quant(bits: int, group: int, scale_dtype: str) -> bq_quant:
     q = bq_quant()
     q.bits, q.group, q.scale_dtype = bits, group, DTYPE_CODES[scale_dtype]
     return q
+
+
+def alloc_rows_quant8(rows: int, cols: int, scale_dtype: str, device):
+    """Outputs of bq_rows_quant8."""
+    import torch
+
+    codes = torch.empty((rows, cols), dtype=torch.int8, device=device)
+    return codes, torch.empty(rows, dtype=torch.float16 if scale_dtype == "f16" else torch.float32, device=device)
+
+
+def _row_stride(t, width: int) -> int:
+    """Elements from one row of t, [..., rows, width], to the next; a tensor of one row has none of its own."""
+    _require(t.shape[-1] == width and (width == 1 or t.numel() == 0 or t.stride(-1) == 1), 2,
+             f"rows of {tuple(t.shape)} must have {width} contiguous elements")
+    if t.shape[-2] <= 1:
+        return width
+    _require(t.stride(-2) >= width, 2, f"rows of {tuple(t.shape)} overlap")
+    return t.stride(-2)
+
+
+def _linear_descriptor(rows: int, inputs: int, w, wscale, values, xbits: int, wbits: int) -> bq_linear:
+    _require(w.dim() in (2, 3) and wscale.numel() == w.numel() // max(1, w.shape[-1]), 2,
+             f"w must be [outputs, bytes] or [experts, outputs, bytes] with one scale per row: {tuple(w.shape)}, {tuple(wscale.shape)}")
+    d = bq_linear()
+    d.rows, d.inputs, d.outputs, d.experts = rows, inputs, w.shape[-2], w.shape[0] if w.dim() == 3 else 1
+    d.xbits, d.wbits, d.dtype, d.scale_dtype = xbits, wbits, _dtype_code(values), _dtype_code(wscale)
+    d.ld_w = _row_stride(w, (inputs * wbits + 7) // 8)
+    _require(w.dim() == 2 or d.experts == 1 or w.stride(0) == d.ld_w * d.outputs, 2, "the experts' weights must follow one another")
+    return d
+
+
+def make_linear(x, w, wscale, y, xbits: int = 8, wbits: int = 8, inputs: int = 0) -> bq_linear:
+    """Descriptor for bq_linear_fwd (w: [outputs, bytes of a row]) and bq_linear_grouped_fwd (w: [experts, outputs, bytes]).  x: codes,
+    [rows, bytes]; y: [rows, outputs].  inputs: where the last byte of a row is not full."""
+    inputs = inputs or x.shape[-1] * 8 // xbits
+    d = _linear_descriptor(x.shape[0], inputs, w, wscale, y, xbits, wbits)
+    _require(x.dim() == y.dim() == 2 and y.shape[0] == d.rows, 2, f"x and y must have the same rows: {tuple(x.shape)}, {tuple(y.shape)}")
+    d.ld_x, d.ld_y = _row_stride(x, (inputs * xbits + 7) // 8), _row_stride(y, d.outputs)
+    return d
+
+
+def make_linear_bwd(dy, w, wscale, dx, wbits: int = 8) -> bq_linear:
+    """Descriptor for bq_linear_bwd and bq_linear_grouped_bwd.  dy: [rows, outputs], dx: [rows, inputs], of one type."""
+    d = _linear_descriptor(dy.shape[0], dx.shape[-1], w, wscale, dy, 8, wbits)
+    _require(dy.dim() == dx.dim() == 2 and dx.shape[0] == d.rows and dx.dtype == dy.dtype, 2,
+             f"dy and dx must have the same rows and type: {tuple(dy.shape)}, {tuple(dx.shape)}")
+    d.ld_x, d.ld_y = _row_stride(dx, d.inputs), _row_stride(dy, d.outputs)
+    return d

@@ -6,6 +6,7 @@
 #include <mutex>
 
 #include "bq_internal.h"
+#include "bq_linear.h"
 
 namespace {
 
@@ -408,6 +409,143 @@ bq_status bq_butterfly_bwd_static(const void *x, const void *dy, const void *pla
                                   const bq_rows *rows, void *stream)
 {
     return bwd_common(x, dy, plan, dx, dtheta, nullptr, 0, true, rows, stream, "bq_butterfly_bwd_static");
+}
+
+bq_status bq_rows_quant8(const void *x, int64_t rows, int32_t cols, int64_t ld_x, int32_t dtype, int8_t *codes, int64_t ld_codes,
+                         void *scales, int32_t scale_dtype, void *stream)
+{
+    const char *who = "bq_rows_quant8";
+    if (dtype != BQ_F32 && dtype != BQ_F16 && dtype != BQ_BF16) return fail(BQ_ERR_DTYPE, "%s: unknown dtype %d", who, (int)dtype);
+    if (scale_dtype != BQ_F32 && scale_dtype != BQ_F16) return fail(BQ_ERR_DTYPE, "%s: scale_dtype must be BQ_F32 or BQ_F16", who);
+    if (rows < 0 || rows >= (int64_t)1 << 31 || cols < 1 || cols > 1 << 24)
+        return fail(BQ_ERR_SHAPE, "%s: rows=%lld cols=%d", who, (long long)rows, (int)cols);
+    if (ld_x < cols || ld_codes < cols)
+        return fail(BQ_ERR_SHAPE, "%s: leading dimensions (%lld, %lld) smaller than the row width %d", who, (long long)ld_x,
+                    (long long)ld_codes, (int)cols);
+    const int64_t ld_max = ld_x > ld_codes ? ld_x : ld_codes;
+    if (rows > 0 && ld_max > ((int64_t)1 << 44) / rows) return fail(BQ_ERR_SHAPE, "%s: rows * leading dimension exceeds 2^44", who);
+    if (rows == 0) return ok();
+    if (!x || !codes || !scales) return fail(BQ_ERR_NULL, "%s: pointer is NULL", who);
+    if (misaligned(x, itemsize(dtype)) || misaligned(scales, itemsize(scale_dtype)))
+        return fail(BQ_ERR_ALIGN, "%s: data pointer not aligned to its element size", who);
+    hipError_t e = bq::launch_row_quant(x, rows, cols, ld_x, dtype, codes, ld_codes, scales, scale_dtype == BQ_F16, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, who);
+    return ok();
+}
+
+// What the calls on a bq_linear descriptor have in common.
+static bq_status check_linear(const bq_linear *d, bool grouped, bool backward, const char *who)
+{
+    if (!d) return fail(BQ_ERR_NULL, "%s: descriptor is NULL", who);
+    if (d->dtype != BQ_F32 && d->dtype != BQ_F16 && d->dtype != BQ_BF16)
+        return fail(BQ_ERR_DTYPE, "%s: unknown dtype %d", who, (int)d->dtype);
+    if (d->scale_dtype != BQ_F32 && d->scale_dtype != BQ_F16)
+        return fail(BQ_ERR_DTYPE, "%s: scale_dtype must be BQ_F32 or BQ_F16", who);
+    if ((d->wbits != 8 && d->wbits != 4 && d->wbits != 2) || (!backward && d->xbits != 8 && d->xbits != 4))
+        return fail(BQ_ERR_UNSUPPORTED, "%s: xbits=%d wbits=%d (8 or 4, and 8, 4 or 2, are implemented)", who, (int)d->xbits, (int)d->wbits);
+    if (d->rows < 0 || d->rows >= (int64_t)1 << 31) return fail(BQ_ERR_SHAPE, "%s: rows=%lld", who, (long long)d->rows);
+    if (d->inputs < 1 || d->inputs > 131071) return fail(BQ_ERR_SHAPE, "%s: inputs=%d outside [1, 131071]", who, (int)d->inputs);
+    const int most = backward ? 131071 : 1 << 24;
+    if (d->outputs < 1 || d->outputs > most) return fail(BQ_ERR_SHAPE, "%s: outputs=%d outside [1, %d]", who, (int)d->outputs, most);
+    if (d->experts < 1 || d->experts > 4096 || (!grouped && d->experts != 1))
+        return fail(BQ_ERR_SHAPE, "%s: experts=%d", who, (int)d->experts);
+    const int64_t x_least = backward ? d->inputs : ((int64_t)d->inputs * d->xbits + 7) / 8;
+    const int64_t w_least = ((int64_t)d->inputs * d->wbits + 7) / 8;
+    if (d->ld_x < x_least || d->ld_w < w_least || d->ld_y < d->outputs)
+        return fail(BQ_ERR_SHAPE, "%s: leading dimensions (%lld, %lld, %lld) smaller than the rows", who, (long long)d->ld_x,
+                    (long long)d->ld_w, (long long)d->ld_y);
+    const int64_t ld_max = d->ld_x > d->ld_y ? d->ld_x : d->ld_y;
+    if ((d->rows > 0 && ld_max > ((int64_t)1 << 44) / d->rows) || d->ld_w > ((int64_t)1 << 44) / ((int64_t)d->experts * d->outputs))
+        return fail(BQ_ERR_SHAPE, "%s: rows * leading dimension exceeds 2^44", who);
+    // one workgroup per 64 x 64 results at most, counted in 31 bits
+    const int64_t width = backward ? d->inputs : d->outputs;
+    if ((d->rows / 64 + d->experts) * ((width + 63) / 64) >= (int64_t)1 << 31) return fail(BQ_ERR_SHAPE, "%s: batch too large", who);
+    return BQ_OK;
+}
+
+static bq_status linear_fwd(bool grouped, const void *x, const void *xscale, const void *w, const void *wscale, const void *bias,
+                            const int32_t *offsets, void *y, const bq_linear *d, void *stream, const char *who)
+{
+    bq_status st = check_linear(d, grouped, false, who);
+    if (st != BQ_OK) return st;
+    if (d->rows == 0) return ok();
+    if (!x || !xscale || !w || !wscale || !y || (grouped && !offsets)) return fail(BQ_ERR_NULL, "%s: pointer is NULL", who);
+    const int scale_size = itemsize(d->scale_dtype), size = itemsize(d->dtype);
+    if (misaligned(xscale, scale_size) || misaligned(wscale, scale_size) || misaligned(y, size) || misaligned(bias, size) ||
+        misaligned(offsets, 4))
+        return fail(BQ_ERR_ALIGN, "%s: data pointer not aligned to its element size", who);
+    bq::LinearArgs A{};
+    A.x = (const uint8_t *)x;
+    A.w = (const uint8_t *)w;
+    A.xs = xscale;
+    A.ws = wscale;
+    A.bias = bias;
+    A.y = y;
+    A.offsets = offsets;
+    A.rows = d->rows;
+    A.ldx = d->ld_x;
+    A.ldw = d->ld_w;
+    A.ldy = d->ld_y;
+    A.w_step = d->outputs * d->ld_w;
+    A.k = d->inputs;
+    A.n = d->outputs;
+    A.experts = d->experts;
+    A.xs_f16 = A.ws_f16 = d->scale_dtype == BQ_F16;
+    A.dtype = d->dtype;
+    hipError_t e = bq::launch_linear(A, d->xbits, d->wbits, 1, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, who);
+    return ok();
+}
+
+bq_status bq_linear_fwd(const void *x, const void *xscale, const void *w, const void *wscale, const void *bias, void *y,
+                        const bq_linear *desc, void *stream)
+{
+    return linear_fwd(false, x, xscale, w, wscale, bias, nullptr, y, desc, stream, "bq_linear_fwd");
+}
+
+bq_status bq_linear_grouped_fwd(const void *x, const void *xscale, const void *w, const void *wscale, const void *bias,
+                                const int32_t *offsets, void *y, const bq_linear *desc, void *stream)
+{
+    return linear_fwd(true, x, xscale, w, wscale, bias, offsets, y, desc, stream, "bq_linear_grouped_fwd");
+}
+
+size_t bq_linear_bwd_workspace_bytes(const bq_linear *desc)
+{
+    if (check_linear(desc, true, true, "bq_linear_bwd_workspace_bytes") != BQ_OK) return 0;
+    g_err[0] = '\0';
+    return bq::linear_bwd_layout(desc->rows, desc->outputs, desc->inputs, desc->experts, desc->dtype).total;
+}
+
+static bq_status linear_bwd(bool grouped, const void *dy, const void *w, const void *wscale, const int32_t *offsets, void *dx,
+                            void *workspace, size_t workspace_bytes, const bq_linear *d, void *stream, const char *who)
+{
+    bq_status st = check_linear(d, grouped, true, who);
+    if (st != BQ_OK) return st;
+    if (d->rows == 0) return ok();
+    if (!dy || !w || !wscale || !dx || !workspace || (grouped && !offsets)) return fail(BQ_ERR_NULL, "%s: pointer is NULL", who);
+    const int size = itemsize(d->dtype);
+    if (misaligned(wscale, itemsize(d->scale_dtype)) || misaligned(dy, size) || misaligned(dx, size) || misaligned(offsets, 4))
+        return fail(BQ_ERR_ALIGN, "%s: data pointer not aligned to its element size", who);
+    if (misaligned(workspace, 256)) return fail(BQ_ERR_ALIGN, "%s: workspace must be aligned to 256 bytes", who);
+    const size_t need = bq::linear_bwd_layout(d->rows, d->outputs, d->inputs, d->experts, d->dtype).total;
+    if (workspace_bytes < need)
+        return fail(BQ_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", who, workspace_bytes, need);
+    hipError_t e = bq::launch_linear_bwd(dy, d->ld_y, w, d->wbits, d->ld_w, wscale, d->scale_dtype == BQ_F16, offsets, dx, d->ld_x,
+                                         workspace, d->rows, d->outputs, d->inputs, d->experts, d->dtype, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, who);
+    return ok();
+}
+
+bq_status bq_linear_bwd(const void *dy, const void *w, const void *wscale, void *dx, void *workspace, size_t workspace_bytes,
+                        const bq_linear *desc, void *stream)
+{
+    return linear_bwd(false, dy, w, wscale, nullptr, dx, workspace, workspace_bytes, desc, stream, "bq_linear_bwd");
+}
+
+bq_status bq_linear_grouped_bwd(const void *dy, const void *w, const void *wscale, const int32_t *offsets, void *dx, void *workspace,
+                                size_t workspace_bytes, const bq_linear *desc, void *stream)
+{
+    return linear_bwd(true, dy, w, wscale, offsets, dx, workspace, workspace_bytes, desc, stream, "bq_linear_grouped_bwd");
 }
 
 const char *bq_status_string(bq_status s)

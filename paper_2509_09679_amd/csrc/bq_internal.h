@@ -253,6 +253,20 @@ hipError_t launch_residual_split(const float *e, int64_t rows, int cols, void *p
 hipError_t launch_quant_grad(const void *v, const void *vq, float *g, const float *factor, const Shape &s, int bits, int group,
                              hipStream_t stream);
 
+// INT8 codes and a scale per row (bq_rowquant.hip)
+hipError_t launch_row_quant(const void *x, int64_t rows, int cols, int64_t ld_x, int dtype, int8_t *codes, int64_t ld_codes, void *scales,
+                            int scale_f16, hipStream_t stream);
+
+// products of codes: bq_linear.h; their gradient: bq_linear_bwd.hip
+struct LinearArgs;
+struct LinearBwdLayout {
+    size_t factor, planes, weights, total;  // offsets into the workspace
+};
+LinearBwdLayout linear_bwd_layout(int64_t rows, int n, int k, int experts, int dtype);
+hipError_t launch_linear_bwd(const void *dy, int64_t ld_dy, const void *w, int wbits, int64_t ldw, const void *ws, int ws_f16,
+                             const int32_t *offsets, void *dx, int64_t ld_dx, void *workspace, int64_t rows, int n, int k, int experts,
+                             int dtype, hipStream_t stream);
+
 // plan build: bq_plan.hip
 hipError_t launch_plan_build(const float *theta, int n, int heads, int k, void *plan, hipStream_t stream);
 

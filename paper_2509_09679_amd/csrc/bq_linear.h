@@ -1,0 +1,129 @@
+// Products of quantised rows with quantised weights: what the translation units share.
+//
+//     y[t, o] = xs[t] ws[o] sum_k x[t, k] w[o, k] + bias[o]
+//
+// x and w are codes of 8, 4 or 2 bits, summed in int32 on the matrix cores (v_mfma_i32_16x16x64_i8): exact, in whatever order,
+// as |x w| <= 2^14 and k < 2^17.  Packed codes are not sign-extended: a field is moved to the top of a byte, which makes it 16
+// (4 bits) or 64 (2 bits) times its value, and the epilogue's factor takes that out again (exact, a power of two).
+//
+// The gradient of the rows, dx[t, k] = sum_o dy[t, o] ws[o] w[o, k], is the same product: dy ws is written as a fixed-point
+// number relative to the row's largest entry, in `planes` base-256 digits of 8 bits, plane 0 the highest; a tile takes the
+// product of every plane and the epilogue joins them.
+//
+// The matrix instruction's first operand is the weights: a lane then holds consecutive channels of one token.
+#pragma once
+
+#include "bq_device.h"
+
+namespace bq {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
+struct LinearArgs {
+    const uint8_t *x, *w;
+    const void *xs, *ws, *bias;  // ws may be NULL (1), bias may be NULL (0)
+    void *y;
+    const int32_t *offsets;  // [experts + 1], NULL: one expert that has all rows
+    int64_t rows, ldx, ldw, ldy;  // ldx, ldw in bytes, ldy in elements
+    int64_t w_step, plane_step;   // bytes from one expert's weights to the next one's, from one plane of x to the next
+    int k, n, experts;
+    int xs_f16, ws_f16, dtype;
+    float factor;  // of the fields' positions
+};
+
+// Rows of one expert that a workgroup takes: [row0, row_end), at most the tile's.
+struct RowTile {
+    int expert;
+    int64_t row0, row_end;
+};
+
+// offsets come from the device: whatever they hold, a range stays within [0, rows]
+__device__ __forceinline__ void expert_rows(const LinearArgs &A, int e, int64_t *a, int64_t *b)
+{
+    if (!A.offsets) {
+        *a = 0;
+        *b = A.rows;
+        return;
+    }
+    const int64_t lo = A.offsets[e], hi = A.offsets[e + 1];
+    *a = lo < 0 ? 0 : lo > A.rows ? A.rows : lo;
+    *b = hi < *a ? *a : hi > A.rows ? A.rows : hi;
+}
+
+// The m-th tile of `tile` rows, counted over all experts (every expert's last one may be short); row0 == row_end behind the last.
+// The lanes of a wave look at 64 experts at a time.
+__device__ __forceinline__ RowTile row_tile(const LinearArgs &A, int64_t m, int tile)
+{
+    RowTile r;
+    if (!A.offsets) {
+        r.expert = 0;
+        r.row0 = m * tile < A.rows ? m * tile : A.rows;
+        r.row_end = r.row0 + tile < A.rows ? r.row0 + tile : A.rows;
+        return r;
+    }
+    r.expert = 0;
+    r.row0 = r.row_end = 0;
+    const int lane = threadIdx.x & 63;
+    for (int base = 0; base < A.experts; base += 64) {
+        int64_t a = 0, b = 0;
+        if (base + lane < A.experts) expert_rows(A, base + lane, &a, &b);
+        const int mine = (int)((b - a + tile - 1) / tile);
+        int upto = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(upto, d, 64);
+            if (lane >= d) upto += o;
+        }
+        const int all = __shfl(upto, 63, 64);
+        if (m < all) {
+            const int at = __ffsll((unsigned long long)__ballot(m < upto)) - 1;  // the first lane whose tiles reach beyond m
+            const int64_t before = __shfl(upto - mine, at, 64);
+            const int64_t ea = ((int64_t)__shfl((int)(a >> 32), at, 64) << 32) | (uint32_t)__shfl((int)a, at, 64);
+            const int64_t eb = ((int64_t)__shfl((int)(b >> 32), at, 64) << 32) | (uint32_t)__shfl((int)b, at, 64);
+            r.expert = base + at;
+            r.row0 = ea + (m - before) * tile;
+            r.row_end = r.row0 + tile < eb ? r.row0 + tile : eb;
+            return r;
+        }
+        m -= all;
+    }
+    return r;
+}
+
+// an upper bound of the number of tiles that the host can state
+inline int64_t row_tiles_bound(const LinearArgs &A, int tile)
+{
+    if (!A.offsets) return (A.rows + tile - 1) / tile;
+    return A.rows / tile + (A.experts < A.rows ? A.experts : A.rows);
+}
+
+__device__ __forceinline__ float load_scale(const void *p, int64_t at, int f16)
+{
+    return f16 ? __half2float(((const __half *)p)[at]) : ((const float *)p)[at];
+}
+
+__device__ __forceinline__ float load_row_value(const void *p, int64_t at, int dtype)
+{
+    if (dtype == BQ_F32) return ((const float *)p)[at];
+    if (dtype == BQ_F16) return __half2float(((const __half *)p)[at]);
+    return to_float(((const bf16_t *)p)[at]);
+}
+
+__device__ __forceinline__ void store_row_value(void *p, int64_t at, int dtype, float v)
+{
+    if (dtype == BQ_F32)
+        ((float *)p)[at] = v;
+    else if (dtype == BQ_F16)
+        ((__half *)p)[at] = __float2half_rn(v);
+    else
+        ((bf16_t *)p)[at] = from_float<bf16_t>(v);
+}
+
+// ---- launchers --------------------------------------------------------------------------------------------
+hipError_t launch_linear_any(const LinearArgs &A, int xbits, int wbits, int planes, hipStream_t stream);  // bq_linear_any.hip
+int64_t linear_any_blocks(const LinearArgs &A);
+// picks the kernel; planes: 1 for codes, 2 or 3 for a gradient's digits (bq_linear.hip)
+hipError_t launch_linear(const LinearArgs &A, int xbits, int wbits, int planes, hipStream_t stream);
+
+}  // namespace bq

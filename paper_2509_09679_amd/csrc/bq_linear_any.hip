@@ -1,0 +1,101 @@
+// The product for any width, stride and alignment: a workgroup of four waves takes 64 tokens x 64 channels, its threads fetch the
+// codes one by one and lay them out as bytes in LDS.  Bound by those loads; the shapes of real layers go to the other kernels.
+#include "bq_linear.h"
+
+namespace bq {
+
+namespace {
+
+constexpr int kTile = 64, kStep = 64, kLd = kStep + 16;  // (rows 80 bytes apart: the 16-byte reads of 16 rows spread over the banks)
+
+__device__ __forceinline__ uint8_t code_at(const uint8_t *row, int k, int bits)
+{
+    if (bits == 8) return row[k];
+    if (bits == 4) return (uint8_t)((row[k >> 1] >> ((k & 1) * 4)) << 4);
+    return (uint8_t)((row[k >> 2] >> ((k & 3) * 2)) << 6);
+}
+
+template <int kPlanes>
+__global__ __launch_bounds__(256) void linear_any_kernel(LinearArgs A, int xbits, int wbits)
+{
+    __shared__ __align__(16) uint8_t s_x[kTile * kLd], s_w[kTile * kLd];
+    const int n_tiles = (A.n + kTile - 1) / kTile;
+    const RowTile rt = row_tile(A, blockIdx.x / n_tiles, kTile);
+    if (rt.row0 >= rt.row_end) return;
+    const int o0 = (int)(blockIdx.x % n_tiles) * kTile;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int to = (wave & 1) * 32, tt = (wave >> 1) * 32;  // this wave's 32 channels x 32 tokens
+    const int r16 = lane & 15, kq = (lane >> 4) * 16;
+    const int srow = tid >> 2, sk = (tid & 3) * 16;  // the 16 codes this thread fetches
+    const int64_t token = rt.row0 + srow;
+    const bool has_token = token < rt.row_end, has_channel = o0 + srow < A.n;
+    const uint8_t *wrow = A.w + rt.expert * A.w_step + (int64_t)(o0 + srow) * A.ldw;
+    int64_t total[2][2][4] = {};
+#pragma unroll
+    for (int p = 0; p < kPlanes; ++p) {
+        const uint8_t *xrow = A.x + p * A.plane_step + token * A.ldx;
+        i32x4 acc[2][2] = {};
+        for (int k0 = 0; k0 < A.k; k0 += kStep) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int k = k0 + sk + j;
+                s_x[srow * kLd + sk + j] = has_token && k < A.k ? code_at(xrow, k, xbits) : 0;
+                s_w[srow * kLd + sk + j] = has_channel && k < A.k ? code_at(wrow, k, wbits) : 0;
+            }
+            __syncthreads();
+            i32x4 w[2], x[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                w[i] = *(const i32x4 *)(s_w + (to + 16 * i + r16) * kLd + kq);
+                x[i] = *(const i32x4 *)(s_x + (tt + 16 * i + r16) * kLd + kq);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i], x[j], acc[i][j], 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) total[i][j][r] = total[i][j][r] * 256 + acc[i][j][r];
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int64_t t = rt.row0 + tt + 16 * j + r16;
+        if (t >= rt.row_end) continue;
+        const float xs = load_scale(A.xs, t, A.xs_f16) * A.factor;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int o = o0 + to + 16 * i + (lane >> 4) * 4 + r;
+                if (o >= A.n) continue;
+                const int64_t at = (int64_t)rt.expert * A.n + o;
+                float v = (float)total[i][j][r] * xs;
+                if (A.ws) v *= load_scale(A.ws, at, A.ws_f16);
+                if (A.bias) v += load_row_value(A.bias, at, A.dtype);
+                store_row_value(A.y, t * A.ldy + o, A.dtype, v);
+            }
+    }
+}
+
+}  // namespace
+
+int64_t linear_any_blocks(const LinearArgs &A) { return row_tiles_bound(A, kTile) * ((A.n + kTile - 1) / kTile); }
+
+hipError_t launch_linear_any(const LinearArgs &A, int xbits, int wbits, int planes, hipStream_t stream)
+{
+    const dim3 grid((unsigned)linear_any_blocks(A));
+    if (planes == 1)
+        hipLaunchKernelGGL(linear_any_kernel<1>, grid, dim3(256), 0, stream, A, xbits, wbits);
+    else if (planes == 2)
+        hipLaunchKernelGGL(linear_any_kernel<2>, grid, dim3(256), 0, stream, A, xbits, wbits);
+    else
+        hipLaunchKernelGGL(linear_any_kernel<3>, grid, dim3(256), 0, stream, A, xbits, wbits);
+    return hipGetLastError();
+}
+
+}  // namespace bq

@@ -6,7 +6,7 @@
  *   i  int32, u  size_t: Python integers; a call with anything else there goes to `general`, which takes what a ctypes prototype takes
  *      (numpy's integers, objects with __index__) and refuses the rest
  *   s  stream handle: a Python integer
- *   r, q  host descriptors: instances of the two ctypes structures the module is given, passed by address
+ *   r, q  host descriptors: instances of the two ctypes structures the Caller is given, passed by address; l: the first of them, a bq_linear
  */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -16,15 +16,16 @@
 
 #include "bq.h"
 
-enum { kMaxArgs = 9 };
+enum { kMaxArgs = 10 };
 typedef union {
     void *p;
     uint64_t u;
 } Arg;
 
 /* kinds of the entry points' arguments, one per prototype */
-static const char *const kKinds[] = {"piipus", "ppprs", "ppppqrs", "pppiprs", "ppppppurs"};
-enum { kPrototypes = 5 };
+static const char *const kKinds[] = {"piipus", "ppprs", "ppppqrs", "pppiprs", "ppppppurs", "puiuipupis", "ppppppls",
+                                     "pppppppls", "pppppuls", "ppppppuls"};
+enum { kPrototypes = 10 };
 
 typedef struct {
     PyObject_HEAD
@@ -32,7 +33,7 @@ typedef struct {
     int prototype; /* of kKinds */
     int count;
     char kinds[kMaxArgs + 1];
-    PyObject *types[2]; /* of 'r' and 'q' */
+    PyObject *types[2]; /* of 'r' or 'l', and of 'q' */
     PyObject *general;
     vectorcallfunc vectorcall;
 } Caller;
@@ -46,7 +47,16 @@ static bq_status invoke(void *f, int prototype, const Arg *a)
         case 1: return ((__typeof__(&bq_butterfly_fwd))f)(a[0].p, a[1].p, a[2].p, a[3].p, a[4].p);
         case 2: return ((__typeof__(&bq_butterfly_fwd_quant))f)(a[0].p, a[1].p, a[2].p, a[3].p, a[4].p, a[5].p, a[6].p);
         case 3: return ((__typeof__(&bq_kron_fwd))f)(a[0].p, a[1].p, a[2].p, (int32_t)a[3].u, a[4].p, a[5].p, a[6].p);
-        default: return ((__typeof__(&bq_butterfly_bwd))f)(a[0].p, a[1].p, a[2].p, a[3].p, a[4].p, a[5].p, (size_t)a[6].u, a[7].p, a[8].p);
+        case 4: return ((__typeof__(&bq_butterfly_bwd))f)(a[0].p, a[1].p, a[2].p, a[3].p, a[4].p, a[5].p, (size_t)a[6].u, a[7].p, a[8].p);
+        case 5:
+            return ((__typeof__(&bq_rows_quant8))f)(a[0].p, (int64_t)a[1].u, (int32_t)a[2].u, (int64_t)a[3].u, (int32_t)a[4].u, a[5].p,
+                                                    (int64_t)a[6].u, a[7].p, (int32_t)a[8].u, a[9].p);
+        case 6: return ((__typeof__(&bq_linear_fwd))f)(a[0].p, a[1].p, a[2].p, a[3].p, a[4].p, a[5].p, a[6].p, a[7].p);
+        case 7:
+            return ((__typeof__(&bq_linear_grouped_fwd))f)(a[0].p, a[1].p, a[2].p, a[3].p, a[4].p, a[5].p, a[6].p, a[7].p, a[8].p);
+        case 8: return ((__typeof__(&bq_linear_bwd))f)(a[0].p, a[1].p, a[2].p, a[3].p, a[4].p, (size_t)a[5].u, a[6].p, a[7].p);
+        default:
+            return ((__typeof__(&bq_linear_grouped_bwd))f)(a[0].p, a[1].p, a[2].p, a[3].p, a[4].p, a[5].p, (size_t)a[6].u, a[7].p, a[8].p);
     }
 }
 
@@ -81,6 +91,7 @@ static PyObject *caller_call(PyObject *self, PyObject *const *args, size_t nargs
                 }
                 break;
             case 'r':
+            case 'l':
             case 'q':
                 if (!PyObject_TypeCheck(o, (PyTypeObject *)c->types[c->kinds[i] == 'q'])) {
                     PyErr_Format(PyExc_TypeError, "argument %d must be a %s", i + 1, ((PyTypeObject *)c->types[c->kinds[i] == 'q'])->tp_name);

@@ -1,0 +1,323 @@
+"""The quantised linear layers on the GPU: every call against the same arithmetic in 64 bits, at the sizes, strides and groups where it
+can go wrong.  The bounds count roundings (tests/linear_util.py)."""
+import numpy as np
+import pytest
+import torch
+
+import linear_util as lu
+from linear_util import DEV, Layer, TORCH
+from paper_2509_09679_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- INT8 codes per row -------------------------------------------------------------------------------
+
+
+def _quant8_reference(x, scale):
+    """The steps of the contract in numpy float32."""
+    v = x.float().cpu().numpy()
+    s = np.abs(v).max(1) / np.float32(127.0)
+    if scale == "f16":
+        s = np.minimum(s, np.float32(65504.0)).astype(np.float16).astype(np.float32)
+    s = np.where(s < np.float32(2.0 ** -126), np.float32(0.0), s)
+    with np.errstate(divide="ignore"):
+        inv = np.where(s == 0, np.float32(0.0), np.float32(1.0) / s)
+    q = np.clip(np.rint(v * inv[:, None]), -128, 127).astype(np.int8)
+    return q, s
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (5, 8), (1, 4096), (37, 512), (9, 520), (6, 1024), (7, 1032), (4, 2048), (5, 2056), (2, 5120),
+                                       (3, 8200), (2, 16384), (2, 16392), (1, 32768), (2, 32776), (3, 11008), (1030, 40)])
+def test_rows_quant8_is_bit_exact(dtype, rows, cols):
+    rng = np.random.default_rng([rows, cols, len(dtype)])
+    for scale, pad, shift in (("f32", 0, 0), ("f16", 8, 0), ("f32", 3, 1)):
+        v = rng.standard_t(3, size=(rows, cols)) * np.exp(rng.normal(size=(rows, 1)) * 3)
+        x = lu.strided(torch.from_numpy(np.clip(v, -6e4, 6e4)).to(TORCH[dtype]), pad, shift)
+        codes = lu.strided(np.full((rows, cols), 77, dtype=np.int8), pad, shift)
+        scales = torch.empty(rows, dtype=TORCH[scale], device=DEV)
+        B.bq_rows_quant8(x, codes, scales)
+        q, s = _quant8_reference(x, scale)
+        np.testing.assert_array_equal(scales.float().cpu().numpy(), s)
+        np.testing.assert_array_equal(codes.cpu().numpy(), q)
+        if pad and rows > 1:  # what lies between the rows stays
+            gap = codes.as_strided((rows - 1, pad), (cols + pad, 1), codes.storage_offset() + cols)
+            assert (gap == 7).all()
+
+
+@pytest.mark.parametrize("cols", [5, 64, 1024, 5120, 40000])
+def test_rows_quant8_special_rows(cols):
+    x = torch.randn(7, cols, device=DEV)
+    x[0] = 0
+    x[1, cols // 2] = float("inf")
+    x[2, cols - 1] = float("nan")
+    x[3] *= 2.0 ** -124  # a scale below 2^-126
+    x[4] *= 2.0 ** -100
+    x[5, 0] = -float("inf")
+    codes, scales = B.alloc_rows_quant8(7, cols, "f32", DEV)
+    B.bq_rows_quant8(x, codes, scales)
+    for r in (0, 3):
+        assert scales[r] == 0 and (codes[r] == 0).all()
+    for r in (1, 2, 5):
+        assert torch.isnan(scales[r]) and (codes[r] == 0).all()
+    for r in (4, 6):
+        assert codes[r].abs().max() == 127
+        assert (codes[r].double() * scales[r].double() - x[r].double()).abs().max() <= scales[r].double() * (0.5 + 1e-5)
+    half = torch.empty(7, dtype=torch.float16, device=DEV)
+    B.bq_rows_quant8(x * 3e7, codes, half)  # beyond binary16: saturates
+    assert half[6] == 65504 and torch.isnan(half[1])
+
+
+def test_rows_quant8_of_no_rows():
+    codes, scales = B.alloc_rows_quant8(0, 64, "f32", DEV)
+    B.bq_rows_quant8(torch.empty(0, 64, device=DEV), codes, scales)
+
+
+# ---- products ------------------------------------------------------------------------------------------
+
+SIZES = [(1, 1, 1), (1, 16, 64), (2, 100, 37), (5, 33, 128), (16, 64, 256), (17, 48, 320), (31, 256, 64), (33, 130, 1024), (64, 257, 192),
+         (65, 512, 448), (100, 1000, 144), (128, 128, 128), (129, 384, 640), (257, 300, 832), (300, 520, 2048), (513, 264, 16)]
+BITS = [(8, 8), (8, 4), (8, 2), (4, 8), (4, 4), (4, 2)]
+
+
+@pytest.mark.parametrize("xbits,wbits", BITS)
+@pytest.mark.parametrize("T,N,K", SIZES)
+def test_linear_fwd(T, N, K, xbits, wbits):
+    rng = np.random.default_rng([T, N, K, xbits, wbits])
+    for dtype, scale, bias in (("f32", "f32", True), ("f16", "f16", False), ("bf16", "f32", True)):
+        L = Layer(rng, T, N, K, xbits=xbits, wbits=wbits, dtype=dtype, scale=scale, bias=bias)
+        want, size = lu.reference_fwd(L.qx, L.xs, L.qw, L.ws, L.bias, [0, T])
+        lu.check(lu.f64(L.forward()), want, lu.bound_fwd(want, size, dtype), f"{dtype}")
+
+
+@pytest.mark.parametrize("T,N,K", [(4, 40, 96), (70, 200, 512), (300, 264, 256)])
+@pytest.mark.parametrize("pads", [(16, 16, 8, 0), (1, 3, 1, 1), (0, 0, 5, 0), (32, 0, 0, 16), (0, 0, 0, 5)])
+def test_linear_fwd_strides_and_alignment(T, N, K, pads):
+    rng = np.random.default_rng([T, N, K, *pads])
+    for bits in ((8, 8), (4, 2)):
+        L = Layer(rng, T, N, K, xbits=bits[0], wbits=bits[1], dtype="f16", bias=True, pad_x=pads[0], pad_w=pads[1], pad_y=pads[2], shift=pads[3])
+        y = L.forward()
+        want, size = lu.reference_fwd(L.qx, L.xs, L.qw, L.ws, L.bias, [0, T])
+        lu.check(lu.f64(y), want, lu.bound_fwd(want, size, "f16"), f"{bits}")
+        if pads[2]:
+            gap = y.as_strided((T - 1, pads[2]), (N + pads[2], 1), y.storage_offset() + N)
+            assert (gap == 7).all()
+
+
+def test_linear_fwd_extreme_sums():
+    # every product +2^14 over the widest rows: the sum reaches 131071 * 2^14, the last one that 32 bits hold
+    for K, bits in ((131071, (8, 8)), (131008, (8, 8)), (131008, (4, 4)), (131008, (8, 2))):
+        lo = [-(1 << (b - 1)) for b in bits]
+        x = torch.from_numpy(lu.pack(np.full((3, K), lo[0]), bits[0])).to(DEV)
+        w = torch.from_numpy(lu.pack(np.full((18, K), lo[1]), bits[1])).to(DEV)
+        one, y = torch.ones(18, device=DEV), torch.empty(3, 18, device=DEV)
+        B.bq_linear_fwd(x, one[:3], w, one, None, y, B.make_linear(x, w, one, y, xbits=bits[0], wbits=bits[1], inputs=K))
+        assert (y == float(np.float32(K * lo[0] * lo[1]))).all()
+
+
+def test_linear_fwd_scales_carry_nan_and_zero():
+    rng = np.random.default_rng(5)
+    L = Layer(rng, 40, 64, 128, dtype="f32")
+    L.xs[3], L.ws[7], L.xs[5] = float("nan"), 0.0, 0.0
+    y = L.forward()
+    assert torch.isnan(y[3]).all() and (y[5] == 0).all() and (y[:3, 7] == 0).all() and torch.isfinite(y[4]).all()
+
+
+GROUPS = [
+    (40, [0, 40]),
+    (40, [0, 0, 40, 40]),
+    (64, [0, 1, 1, 18, 64]),
+    (96, [5, 21, 22, 90]),  # rows before the first and behind the last expert
+    (300, [0, 3, 3, 150, 151, 290, 290, 290, 300]),
+    (700, [0, 0, 690, 700]),
+    (30, [7] * 71 + [20] * 60),  # more experts than a wave looks at at once
+    (1, [0, 0, 1]),
+]
+
+
+@pytest.mark.parametrize("N,K", [(40, 64), (200, 37), (264, 384)])
+@pytest.mark.parametrize("T,offsets", GROUPS)
+def test_grouped_fwd(T, offsets, N, K):
+    rng = np.random.default_rng([T, len(offsets), N, K])
+    for dtype, bits, bias in (("bf16", (8, 8), True), ("f32", (4, 4), False), ("f16", (8, 2), True)):
+        L = Layer(rng, T, N, K, E=len(offsets) - 1, xbits=bits[0], wbits=bits[1], dtype=dtype, bias=bias)
+        y = lu.f64(L.forward(lu.offsets_tensor(offsets)))
+        want, size = lu.reference_fwd(L.qx, L.xs, L.qw, L.ws, L.bias, offsets)
+        a, b = offsets[0], offsets[-1]
+        lu.check(y[a:b], want[a:b], lu.bound_fwd(want, size, dtype)[a:b], f"{dtype}")
+        assert (y[:a] == 3).all() and (y[b:] == 3).all()  # rows of no expert are left as they were
+
+
+def test_grouped_offsets_outside_the_batch_are_taken_as_the_nearest_inside():
+    rng = np.random.default_rng(8)
+    L = Layer(rng, 50, 70, 64, E=3, dtype="f32")
+    y = lu.f64(L.forward(lu.offsets_tensor([-9, 20, 45, 4000])))
+    want, size = lu.reference_fwd(L.qx, L.xs, L.qw, L.ws, L.bias, [0, 20, 45, 50])
+    lu.check(y, want, lu.bound_fwd(want, size, "f32"), "clamped")
+
+
+# ---- gradients -----------------------------------------------------------------------------------------
+
+
+def _gradient(rng, T, N, dtype, pad=0):
+    g = rng.standard_t(4, size=(T, N)) * np.exp(rng.normal(size=(T, 1)) * 2) * 1e-3
+    return lu.strided(torch.from_numpy(np.clip(g, -100, 100)).to(TORCH[dtype]), pad)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T,N,K", [(1, 1, 1), (2, 37, 100), (5, 128, 33), (17, 320, 48), (64, 64, 64), (65, 200, 130), (130, 1000, 264), (200, 129, 512),
+                                   (300, 2048, 96)])
+def test_linear_bwd(T, N, K, dtype):
+    rng = np.random.default_rng([T, N, K])
+    for wbits, scale, pad in ((8, "f32", 0), (4, "f16", 8), (2, "f32", 3)):
+        L = Layer(rng, T, N, K, wbits=wbits, dtype=dtype, scale=scale, pad_w=pad, pad_y=pad)
+        dy = _gradient(rng, T, N, dtype, pad)
+        dx = lu.f64(L.backward(dy))
+        want, weight, top = lu.reference_bwd(dy, L.qw, L.ws, [0, T])
+        lu.check(dx, want, lu.bound_bwd(want, weight, top, dtype), f"w{wbits}")
+
+
+@pytest.mark.parametrize("N,K", [(40, 64), (200, 37), (264, 384)])
+@pytest.mark.parametrize("T,offsets", GROUPS)
+def test_grouped_bwd(T, offsets, N, K):
+    rng = np.random.default_rng([T, len(offsets), N, K])
+    for dtype, wbits in (("bf16", 8), ("f32", 4)):
+        L = Layer(rng, T, N, K, E=len(offsets) - 1, wbits=wbits, dtype=dtype)
+        dy = _gradient(rng, T, N, dtype)
+        dx = lu.f64(L.backward(dy, lu.offsets_tensor(offsets)))
+        want, weight, top = lu.reference_bwd(dy, L.qw, L.ws, offsets)
+        a, b = offsets[0], offsets[-1]
+        lu.check(dx[a:b], want[a:b], lu.bound_bwd(want, weight, top, dtype)[a:b], f"{dtype}")
+        assert (dx[:a] == 3).all() and (dx[b:] == 3).all()
+
+
+def test_bwd_is_the_derivative_of_fwd():
+    # <dy, y(x + h e) - y(x - h e)> / 2h along single dequantised entries, which the layer is linear in: one code up, one down
+    rng = np.random.default_rng(11)
+    T, N, K = 6, 50, 40
+    L = Layer(rng, T, N, K, dtype="f32")
+    L.qx = np.clip(L.qx, -120, 120)
+    dy = _gradient(rng, T, N, "f32")
+    dx = lu.f64(L.backward(dy))
+    _, weight, top = lu.reference_bwd(dy, L.qw, L.ws, [0, T])
+    g, xs = lu.f64(dy), lu.f64(L.xs)
+    for t, k in ((0, 0), (3, 17), (5, 39)):
+        sides = []
+        for h in (1, -1):
+            q = L.qx.copy()
+            q[t, k] += h
+            L.x = torch.from_numpy(lu.pack(q, 8)).to(DEV)
+            y = lu.f64(L.forward())
+            sides.append(((g * y).sum(), (np.abs(g * y)).sum()))
+        d = (sides[0][0] - sides[1][0]) / (2 * xs[t])
+        err = lu.bound_bwd(np.array([[dx[t, k]]]), weight[t:t + 1, k:k + 1], top[t:t + 1], "f32")[0, 0]
+        assert abs(d - dx[t, k]) <= err + 5 * 2.0 ** -24 * (sides[0][1] + sides[1][1]) / (2 * xs[t])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_bwd_special_rows(dtype):
+    rng = np.random.default_rng(12)
+    T, N, K = 9, 130, 96
+    L = Layer(rng, T, N, K, dtype=dtype)
+    dy = _gradient(rng, T, N, dtype).clone()
+    dy[0] = 0
+    dy[1, 5] = float("nan")
+    dy[2, 129] = float("inf")
+    dy[3] = dy[4] * 2.0 ** -90   # tiny rows keep their relative accuracy
+    dy[5] = dy[4] * 2.0 ** -119  # ... down to 2^-120
+    dy[6, 1:] = 0                # one entry
+    dx = lu.f64(L.backward(dy))
+    assert (dx[0] == 0).all() and np.isnan(dx[1]).all() and np.isnan(dx[2]).all()
+    want, weight, top = lu.reference_bwd(dy, L.qw, L.ws, [0, T])
+    keep = [3, 4, 6, 7, 8]
+    lu.check(dx[keep], want[keep], lu.bound_bwd(want, weight, top, dtype)[keep], "rows")
+    assert np.isfinite(dx[5]).all() and (np.abs(dx[5] - want[5]) <= 2.0 ** -119 * weight[5]).all()
+
+
+# ---- streams, graphs, a layer as it is used --------------------------------------------------------------
+
+
+def test_captured_calls_replay_bit_exact():
+    rng = np.random.default_rng(13)
+    T, N, K, offsets = 200, 320, 512, [0, 70, 70, 180]
+    x = torch.randn(T, K, device=DEV, dtype=torch.float16)
+    codes, xs = B.alloc_rows_quant8(T, K, "f32", DEV)
+    L, G = Layer(rng, T, N, K, dtype="f16", wbits=4), Layer(rng, T, N, K, E=3, dtype="f16")
+    off = lu.offsets_tensor(offsets)
+    y, yg, dx, dxg = (torch.zeros(T, w, dtype=torch.float16, device=DEV) for w in (N, N, K, K))
+    d, dg = B.make_linear(codes, L.w, L.ws, y, wbits=4), B.make_linear(codes, G.w, G.ws, yg)
+    b, bg = B.make_linear_bwd(y, L.w, L.ws, dx, wbits=4), B.make_linear_bwd(yg, G.w, G.ws, dxg)
+    work, workg = (torch.empty(B.bq_linear_bwd_workspace_bytes(v), dtype=torch.uint8, device=DEV) for v in (b, bg))
+    outs = [codes, xs, y, yg, dx, dxg]
+
+    def sequence():
+        B.bq_rows_quant8(x, codes, xs)
+        B.bq_linear_fwd(codes, xs, L.w, L.ws, None, y, d)
+        B.bq_linear_grouped_fwd(codes, xs, G.w, G.ws, None, off, yg, dg)
+        B.bq_linear_bwd(y, L.w, L.ws, dx, work, b)
+        B.bq_linear_grouped_bwd(yg, G.w, G.ws, off, dxg, workg, bg)
+
+    sequence()
+    torch.cuda.synchronize()
+    want = [o.clone() for o in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        sequence()
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            sequence()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for o in outs[:3] + outs[4:5]:
+            o.fill_(3)
+        yg[:180].fill_(3)
+        dxg[:180].fill_(3)
+        work.fill_(0xA5)
+        workg.fill_(0xA5)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for o, w in zip(outs, want):
+            assert torch.equal(o, w)
+        sequence()
+        torch.cuda.synchronize()
+
+
+def test_calls_go_to_the_stream_they_are_given():
+    rng = np.random.default_rng(14)
+    L = Layer(rng, 33, 64, 128, dtype="f32")
+    want = L.forward()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    y = torch.zeros_like(want)
+    d = B.make_linear(L.x, L.w, L.ws, y)
+    with torch.cuda.stream(side):
+        B.bq_linear_fwd(L.x, L.xs, L.w, L.ws, None, y, d)
+    side.synchronize()
+    assert torch.equal(y, want)
+    y.zero_()
+    torch.cuda.synchronize()
+    B.bq_linear_fwd(L.x, L.xs, L.w, L.ws, None, y, d, stream=side)
+    side.synchronize()
+    assert torch.equal(y, want)
+
+
+def test_two_streams_at_once():
+    rng = np.random.default_rng(15)
+    layers = [Layer(rng, 300, 512, 1024, dtype="bf16", wbits=w) for w in (8, 4)]
+    dys = [_gradient(rng, 300, 512, "bf16") for _ in layers]
+    want = [(L.forward(), L.backward(g)) for L, g in zip(layers, dys)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in layers]
+    got = [[], []]
+    for _ in range(4):
+        for i, (L, g, s) in enumerate(zip(layers, dys, streams)):
+            with torch.cuda.stream(s):
+                got[i].append((L.forward(), L.backward(g)))
+    torch.cuda.synchronize()
+    for i, w in enumerate(want):
+        for y, dx in got[i]:
+            assert torch.equal(y, w[0]) and torch.equal(dx, w[1])

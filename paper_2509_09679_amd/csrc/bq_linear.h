@@ -30,6 +30,7 @@ struct LinearArgs {
     int k, n, experts;
     int xs_f16, ws_f16, dtype;
     float factor;  // of the fields' positions
+    int y_quads;   // rows of y are 16-byte aligned
 };
 
 // Rows of one expert that a workgroup takes: [row0, row_end), at most the tile's.
@@ -49,6 +50,12 @@ __device__ __forceinline__ void expert_rows(const LinearArgs &A, int e, int64_t 
     const int64_t lo = A.offsets[e], hi = A.offsets[e + 1];
     *a = lo < 0 ? 0 : lo > A.rows ? A.rows : lo;
     *b = hi < *a ? *a : hi > A.rows ? A.rows : hi;
+}
+
+// a value that all lanes of the wave hold, in scalar registers
+__device__ __forceinline__ int64_t uniform(int64_t v)
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
 }
 
 // The m-th tile of `tile` rows, counted over all experts (every expert's last one may be short); row0 == row_end behind the last.
@@ -75,15 +82,15 @@ __device__ __forceinline__ RowTile row_tile(const LinearArgs &A, int64_t m, int 
             const int o = __shfl_up(upto, d, 64);
             if (lane >= d) upto += o;
         }
-        const int all = __shfl(upto, 63, 64);
+        const int all = __builtin_amdgcn_readlane(upto, 63);
         if (m < all) {
             const int at = __ffsll((unsigned long long)__ballot(m < upto)) - 1;  // the first lane whose tiles reach beyond m
             const int64_t before = __shfl(upto - mine, at, 64);
             const int64_t ea = ((int64_t)__shfl((int)(a >> 32), at, 64) << 32) | (uint32_t)__shfl((int)a, at, 64);
             const int64_t eb = ((int64_t)__shfl((int)(b >> 32), at, 64) << 32) | (uint32_t)__shfl((int)b, at, 64);
-            r.expert = base + at;
-            r.row0 = ea + (m - before) * tile;
-            r.row_end = r.row0 + tile < eb ? r.row0 + tile : eb;
+            r.expert = __builtin_amdgcn_readfirstlane(base + at);
+            r.row0 = uniform(ea + (m - before) * tile);
+            r.row_end = uniform(ea + (m - before + 1) * tile < eb ? ea + (m - before + 1) * tile : eb);
             return r;
         }
         m -= all;
@@ -91,7 +98,24 @@ __device__ __forceinline__ RowTile row_tile(const LinearArgs &A, int64_t m, int 
     return r;
 }
 
-// an upper bound of the number of tiles that the host can state
+// how many there are
+__device__ __forceinline__ int64_t row_tiles(const LinearArgs &A, int tile)
+{
+    if (!A.offsets) return (A.rows + tile - 1) / tile;
+    const int lane = threadIdx.x & 63;
+    int64_t all = 0;
+    for (int base = 0; base < A.experts; base += 64) {
+        int64_t a = 0, b = 0;
+        if (base + lane < A.experts) expert_rows(A, base + lane, &a, &b);
+        int mine = (int)((b - a + tile - 1) / tile);
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) mine += __shfl_xor(mine, d, 64);
+        all += __builtin_amdgcn_readfirstlane(mine);
+    }
+    return all;
+}
+
+// an upper bound that the host can state
 inline int64_t row_tiles_bound(const LinearArgs &A, int tile)
 {
     if (!A.offsets) return (A.rows + tile - 1) / tile;
@@ -123,6 +147,13 @@ __device__ __forceinline__ void store_row_value(void *p, int64_t at, int dtype, 
 // ---- launchers --------------------------------------------------------------------------------------------
 hipError_t launch_linear_any(const LinearArgs &A, int xbits, int wbits, int planes, hipStream_t stream);  // bq_linear_any.hip
 int64_t linear_any_blocks(const LinearArgs &A);
+// few rows: bq_linear_rows.h; blocks: 16-token blocks of a pass, 1, 2 or 4
+hipError_t launch_linear_rows8(const LinearArgs &A, int wbits, int planes, int blocks, hipStream_t stream);
+hipError_t launch_linear_rows4(const LinearArgs &A, int wbits, int blocks, hipStream_t stream);
+// many: bq_linear_tile.h
+hipError_t launch_linear_tile8(const LinearArgs &A, int wbits, bool large, hipStream_t stream);
+hipError_t launch_linear_tile4(const LinearArgs &A, int wbits, bool large, hipStream_t stream);
+hipError_t launch_linear_tile_digits(const LinearArgs &A, int planes, bool large, hipStream_t stream);
 // picks the kernel; planes: 1 for codes, 2 or 3 for a gradient's digits (bq_linear.hip)
 hipError_t launch_linear(const LinearArgs &A, int xbits, int wbits, int planes, hipStream_t stream);
 

@@ -1,0 +1,97 @@
+// Codes as the matrix cores take them: 16 bytes per lane, from 16 codes of 8, 4 or 2 bits.
+#pragma once
+
+#include "bq_linear.h"
+
+namespace bq {
+
+// 8 codes of 4 bits, as bytes that hold 16 times the code.  Natural order costs a byte interleave; where both operands have 4 bits
+// they can stay in the order (even codes, odd codes), which the sum does not see.
+template <bool kNatural>
+__device__ __forceinline__ void unpack4bit(uint32_t w, uint32_t &lo, uint32_t &hi)
+{
+    const uint32_t even = (w << 4) & 0xF0F0F0F0u, odd = w & 0xF0F0F0F0u;
+    if (kNatural) {
+        lo = __builtin_amdgcn_perm(odd, even, 0x05010400u);
+        hi = __builtin_amdgcn_perm(odd, even, 0x07030602u);
+    } else {
+        lo = even;
+        hi = odd;
+    }
+}
+
+// 16 codes of 2 bits, as bytes that hold 64 times the code, in natural order
+__device__ __forceinline__ i32x4 unpack2bit(uint32_t w)
+{
+    const uint32_t t0 = (w << 6) & 0xC0C0C0C0u, t1 = (w << 4) & 0xC0C0C0C0u, t2 = (w << 2) & 0xC0C0C0C0u, t3 = w & 0xC0C0C0C0u;
+    const uint32_t a = __builtin_amdgcn_perm(t1, t0, 0x05010400u), b = __builtin_amdgcn_perm(t3, t2, 0x05010400u);
+    const uint32_t c = __builtin_amdgcn_perm(t1, t0, 0x07030602u), d = __builtin_amdgcn_perm(t3, t2, 0x07030602u);
+    i32x4 r;
+    r[0] = (int)__builtin_amdgcn_perm(b, a, 0x05040100u);
+    r[1] = (int)__builtin_amdgcn_perm(b, a, 0x07060302u);
+    r[2] = (int)__builtin_amdgcn_perm(d, c, 0x05040100u);
+    r[3] = (int)__builtin_amdgcn_perm(d, c, 0x07060302u);
+    return r;
+}
+
+// the 16 codes of step s out of a lane's packed words (8 bits: 4 words per step; 4 bits: 2; 2 bits: 1)
+template <int kBits, bool kNatural, int kWords>
+__device__ __forceinline__ i32x4 step_codes(const uint32_t (&w)[kWords], int s)
+{
+    i32x4 r;
+    if constexpr (kBits == 8) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] = (int)w[4 * s + j];
+    } else if constexpr (kBits == 4) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            uint32_t lo, hi;
+            unpack4bit<kNatural>(w[2 * s + j], lo, hi);
+            r[2 * j] = (int)lo;
+            r[2 * j + 1] = (int)hi;
+        }
+    } else {
+        r = unpack2bit(w[s]);
+    }
+    return r;
+}
+
+// what the epilogues have in common: the value of one result from its sums (one per plane)
+template <int kPlanes>
+__device__ __forceinline__ float joined(const int (&sum)[kPlanes])
+{
+    if constexpr (kPlanes == 1) return (float)sum[0];
+    if constexpr (kPlanes == 2) return (float)__builtin_fma((double)sum[0], 256.0, (double)sum[1]);
+    if constexpr (kPlanes == 3) return (float)__builtin_fma((double)sum[0], 65536.0, __builtin_fma((double)sum[1], 256.0, (double)sum[2]));
+}
+
+// kCount (a multiple of 4) consecutive results of one row, `left` of them inside the row; vec: 4 results at a time are aligned
+template <int kCount>
+__device__ __forceinline__ void store_results(const LinearArgs &A, int64_t at, const float (&v)[kCount], int left, bool vec)
+{
+    if (vec && left >= kCount) {
+        if (A.dtype == BQ_F32) {
+#pragma unroll
+            for (int j = 0; j < kCount; j += 4) *(float4 *)((float *)A.y + at + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            return;
+        }
+        uint32_t w[kCount / 2];
+#pragma unroll
+        for (int j = 0; j < kCount; j += 2)
+            w[j / 2] = A.dtype == BQ_F16 ? f32x2_to_f16x2_bits(v[j], v[j + 1]) : f32x2_to_bf16x2_bits(v[j], v[j + 1]);
+        uint16_t *p = (uint16_t *)A.y + at;
+        if constexpr (kCount % 8 == 0) {
+#pragma unroll
+            for (int j = 0; j < kCount / 2; j += 4) *(uint4 *)(p + 2 * j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kCount / 2; j += 2) *(uint2 *)(p + 2 * j) = make_uint2(w[j], w[j + 1]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < kCount; ++j)
+        if (j < left) store_row_value(A.y, at + j, A.dtype, v[j]);
+}
+
+}  // namespace bq

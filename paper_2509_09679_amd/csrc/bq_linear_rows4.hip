@@ -1,0 +1,13 @@
+// Few rows of 4-bit codes.
+#include "bq_linear_rows.h"
+
+namespace bq {
+
+hipError_t launch_linear_rows4(const LinearArgs &A, int wbits, int blocks, hipStream_t stream)
+{
+    if (wbits == 8) return launch_rows<4, 8, 1>(A, blocks, stream);
+    if (wbits == 4) return launch_rows<4, 4, 1>(A, blocks, stream);
+    return launch_rows<4, 2, 1>(A, blocks, stream);
+}
+
+}  // namespace bq

@@ -1,0 +1,15 @@
+// Few rows of 8-bit codes, and of a gradient's digits.
+#include "bq_linear_rows.h"
+
+namespace bq {
+
+hipError_t launch_linear_rows8(const LinearArgs &A, int wbits, int planes, int blocks, hipStream_t stream)
+{
+    if (planes == 2) return launch_rows<8, 8, 2>(A, blocks, stream);
+    if (planes == 3) return launch_rows<8, 8, 3>(A, blocks, stream);
+    if (wbits == 8) return launch_rows<8, 8, 1>(A, blocks, stream);
+    if (wbits == 4) return launch_rows<8, 4, 1>(A, blocks, stream);
+    return launch_rows<8, 2, 1>(A, blocks, stream);
+}
+
+}  // namespace bq

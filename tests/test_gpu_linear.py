@@ -321,3 +321,76 @@ def test_two_streams_at_once():
     for i, w in enumerate(want):
         for y, dx in got[i]:
             assert torch.equal(y, w[0]) and torch.equal(dx, w[1])
+
+
+# ---- batches that take the large tiles: references in 64 bits on the device ------------------------------
+
+
+def _codes_on_device(gen, shape, bits):
+    q = torch.randint(-(1 << (bits - 1)), 1 << (bits - 1), shape, generator=gen, device=DEV)
+    per = 8 // bits
+    f = (q & ((1 << bits) - 1)).unflatten(-1, (shape[-1] // per, per))
+    byte = sum(f[..., j] << (bits * j) for j in range(per))
+    return q.double(), torch.where(byte > 127, byte - 256, byte).to(torch.int8)
+
+
+def _within(got, want, bound):
+    err = (got.double() - want).abs()
+    assert (err <= bound).all(), f"{(~(err <= bound)).sum().item()} beyond the bound, the worst by {(err / bound).max().item():.3g}"
+
+
+@pytest.mark.parametrize("xbits,wbits,K", [(8, 8, 208), (8, 4, 416), (8, 2, 192), (4, 8, 160), (4, 4, 1056), (4, 2, 320)])
+@pytest.mark.parametrize("experts", [0, 5])
+def test_large_tiles_fwd(xbits, wbits, K, experts):
+    T, N = (4357, 4200) if not experts else (9001, 2300)
+    gen = torch.Generator(device=DEV).manual_seed(K + experts)
+    offsets = [3, 1500, 1500, 1501, 7000, 8990] if experts else [0, T]
+    E = max(1, experts)
+    qx, x = _codes_on_device(gen, (T, K), xbits)
+    qw, w = _codes_on_device(gen, (E, N, K), wbits)
+    xs, ws = (torch.rand(s, generator=gen, device=DEV) * 0.01 + 1e-3 for s in ((T,), (E, N)))
+    bias = torch.randn((E, N), generator=gen, device=DEV).bfloat16()
+    for dtype in ("bf16", "f32"):
+        b = bias.to(TORCH[dtype])
+        y = torch.full((T, N), 3.0, dtype=TORCH[dtype], device=DEV)
+        if experts:
+            B.bq_linear_grouped_fwd(x, xs, w, ws, b, lu.offsets_tensor(offsets), y, B.make_linear(x, w, ws, y, xbits=xbits, wbits=wbits))
+        else:
+            B.bq_linear_fwd(x, xs, w[0], ws[0], b[0], y, B.make_linear(x, w[0], ws[0], y, xbits=xbits, wbits=wbits))
+        for e in range(E):
+            lo, hi = offsets[e], offsets[e + 1]
+            p = (qx[lo:hi] @ qw[e].t()) * xs[lo:hi, None].double() * ws[e].double()
+            want = p + b[e].double()
+            f32 = 5 * 2.0 ** -24 * (p.abs() + b[e].double().abs())
+            _within(y[lo:hi], want, f32 + (lu.half_step(dtype) * (want.abs() + f32) if dtype != "f32" else 0) + 1e-40)
+        assert (y[:offsets[0]] == 3).all() and (y[offsets[-1]:] == 3).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("experts", [0, 5])
+def test_large_tiles_bwd(dtype, experts):
+    T, N, K = (4357, 200, 4200) if not experts else (9001, 136, 2300)
+    gen = torch.Generator(device=DEV).manual_seed(experts + 1)
+    offsets = [3, 1500, 1500, 1501, 7000, 8990] if experts else [0, T]
+    E = max(1, experts)
+    qw, w = _codes_on_device(gen, (E, N, K), 4)
+    ws = torch.rand((E, N), generator=gen, device=DEV) * 0.01 + 1e-3
+    dy = (torch.randn((T, N), generator=gen, device=DEV) * torch.exp(torch.randn((T, 1), generator=gen, device=DEV))).to(TORCH[dtype])
+    dx = torch.full((T, K), 3.0, dtype=TORCH[dtype], device=DEV)
+    wd, wsd = (w, ws) if experts else (w[0], ws[0])
+    d = B.make_linear_bwd(dy, wd, wsd, dx, wbits=4)
+    work = torch.full((B.bq_linear_bwd_workspace_bytes(d),), 0xA5, dtype=torch.uint8, device=DEV)
+    if experts:
+        B.bq_linear_grouped_bwd(dy, wd, wsd, lu.offsets_tensor(offsets), dx, work, d)
+    else:
+        B.bq_linear_bwd(dy, wd, wsd, dx, work, d)
+    term = 0.5 / lu.QMAX[3 if dtype == "f32" else 2] + 5 * 2.0 ** -24
+    for e in range(E):
+        lo, hi = offsets[e], offsets[e + 1]
+        if lo == hi:
+            continue
+        v = dy[lo:hi].double() * ws[e].double()
+        want = v @ qw[e]
+        f32 = term * v.abs().amax(1, keepdim=True) * qw[e].abs().sum(0) + 2 * 2.0 ** -24 * want.abs()
+        _within(dx[lo:hi], want, f32 + (lu.half_step(dtype) * (want.abs() + f32) if dtype != "f32" else 0) + 1e-40)
+    assert (dx[:offsets[0]] == 3).all() and (dx[offsets[-1]:] == 3).all()

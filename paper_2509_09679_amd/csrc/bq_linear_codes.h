@@ -61,8 +61,42 @@ template <int kPlanes>
 __device__ __forceinline__ float joined(const int (&sum)[kPlanes])
 {
     if constexpr (kPlanes == 1) return (float)sum[0];
-    if constexpr (kPlanes == 2) return (float)__builtin_fma((double)sum[0], 256.0, (double)sum[1]);
+    // (two digits serve 16-bit results: what float32 loses of the lower sum is 2^-17 of the digits' own rounding)
+    if constexpr (kPlanes == 2) return __builtin_fmaf((float)sum[0], 256.0f, (float)sum[1]);
     if constexpr (kPlanes == 3) return (float)__builtin_fma((double)sum[0], 65536.0, __builtin_fma((double)sum[1], 256.0, (double)sum[2]));
+}
+
+// scales and bias of some channels: every type's loads in a branch of its own, so that they are in flight together
+template <int kCount>
+__device__ __forceinline__ void channel_scales(const LinearArgs &A, const int64_t (&at)[kCount], float (&s)[kCount])
+{
+    if (!A.ws) {
+#pragma unroll
+        for (int c = 0; c < kCount; ++c) s[c] = 1.0f;
+    } else if (A.ws_f16) {
+#pragma unroll
+        for (int c = 0; c < kCount; ++c) s[c] = __half2float(((const __half *)A.ws)[at[c]]);
+    } else {
+#pragma unroll
+        for (int c = 0; c < kCount; ++c) s[c] = ((const float *)A.ws)[at[c]];
+    }
+}
+template <int kCount>
+__device__ __forceinline__ void channel_bias(const LinearArgs &A, const int64_t (&at)[kCount], float (&b)[kCount])
+{
+    if (!A.bias) {
+#pragma unroll
+        for (int c = 0; c < kCount; ++c) b[c] = 0.0f;
+    } else if (A.dtype == BQ_F32) {
+#pragma unroll
+        for (int c = 0; c < kCount; ++c) b[c] = ((const float *)A.bias)[at[c]];
+    } else if (A.dtype == BQ_F16) {
+#pragma unroll
+        for (int c = 0; c < kCount; ++c) b[c] = __half2float(((const __half *)A.bias)[at[c]]);
+    } else {
+#pragma unroll
+        for (int c = 0; c < kCount; ++c) b[c] = to_float(((const bf16_t *)A.bias)[at[c]]);
+    }
 }
 
 // kCount (a multiple of 4) consecutive results of one row, `left` of them inside the row; vec: 4 results at a time are aligned

@@ -11,6 +11,8 @@
 // with 16 consecutive channels of one token.
 #pragma once
 
+#include <type_traits>
+
 #include "bq_linear_codes.h"
 
 namespace bq {
@@ -23,16 +25,19 @@ struct TileShape {
     static constexpr int x_rows = kWavesT * kPieces * 16, w_rows = kWavesN * 64;
 };
 
-// f of the header comment; kPieceBytes: bytes of an LDS row.  x rows are read 16 in a row, w rows as i -> 16 (i / 4) + i % 4.
+// f of the header comment.  A read of 16 bytes per lane goes 16 lanes at a time, {0-3, 12-15, 20-27} and {4-11, 16-19, 28-31} of either
+// half of the wave (measured: two lanes that read the same banks cost a cycle exactly if both are in one of these sets), over 64
+// banks: 256 bytes, 2 or 4 LDS rows.  x rows are read 16 in a row, w rows as i -> 16 (i / 4) + i % 4, neighbouring lane groups
+// neighbouring pieces (4 bits) or pairs of them (8 bits).
 template <int kRowBytes>
 __device__ __forceinline__ int x_turn(int row)
 {
-    return kRowBytes == 128 ? row & 7 : (row >> 1) & 3;
+    return kRowBytes == 128 ? ((row >> 1) & 1) | ((row >> 1) & 4) : (row >> 2) & 2;
 }
 template <int kRowBytes>
 __device__ __forceinline__ int w_turn(int row)
 {
-    return kRowBytes == 128 ? (row & 3) | ((row >> 2) & 4) : kRowBytes == 64 ? ((row >> 1) & 1) | ((row >> 3) & 2) : (row >> 4) & 1;
+    return kRowBytes == 128 ? ((row >> 1) & 1) | ((row >> 3) & 4) : kRowBytes == 64 ? (row >> 4) & 2 : (row >> 4) & 1;
 }
 
 __device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, const uint8_t *base)
@@ -54,14 +59,12 @@ __global__ __launch_bounds__(Shape::threads, 1) void linear_tile_kernel(LinearAr
 
     // which tile: workgroups go round the 8 XCDs, each of which takes a contiguous eighth of the tiles; within it 8 tiles along the
     // tokens and then the next channels, so that what runs together shares its rows in the XCD's L2
-    const int n_tiles = (A.n + Shape::w_rows - 1) / Shape::w_rows;
-    const int64_t m_tiles = row_tiles(A, kTokens);
-    const int64_t all = m_tiles * n_tiles, each = (all + 7) / 8;
-    const int64_t idx = blockIdx.x >> 3;
-    const int64_t tile = (int64_t)(blockIdx.x & 7) * each + idx;
+    const uint32_t n_tiles = (uint32_t)(A.n + Shape::w_rows - 1) / Shape::w_rows, m_tiles = (uint32_t)row_tiles(A, kTokens);
+    const uint32_t all = m_tiles * n_tiles, each = (all + 7) / 8, idx = blockIdx.x >> 3;
+    const uint32_t tile = (blockIdx.x & 7) * each + idx;
     if (idx >= each || tile >= all) return;
-    const int64_t band = tile / (8 * n_tiles), in_band = tile - band * (8 * n_tiles);
-    const int64_t band_rows = m_tiles - band * 8 < 8 ? m_tiles - band * 8 : 8;
+    const uint32_t band = tile / (8 * n_tiles), in_band = tile - band * (8 * n_tiles);
+    const uint32_t band_rows = m_tiles - band * 8 < 8 ? m_tiles - band * 8 : 8;
     RowTile rt = row_tile(A, band * 8 + in_band % band_rows, kTokens);
     rt = RowTile{__builtin_amdgcn_readfirstlane(rt.expert), uniform(rt.row0), uniform(rt.row_end)};
     const int o0 = (int)(in_band / band_rows) * Shape::w_rows;
@@ -96,81 +99,128 @@ __global__ __launch_bounds__(Shape::threads, 1) void linear_tile_kernel(LinearAr
     }
     const int stages = (A.k + 127) / 128;
     const int x_tail = (int)((int64_t)A.k * kXBits / 128) % (kXRow / 16), w_tail = (int)((int64_t)A.k * kWBits / 128) % (kWRow / 16);  // pieces of the last stage
-    auto load_stage = [&](int s) {
+    constexpr int kLoads = kXLoads + kWLoads;
+    auto load = [&](int s, int n) {  // the n-th of a stage's loads
         const uint32_t at = lds0 + (s & 1) * kStage + wave * 1024;
-        const bool short_x = x_tail && s == stages - 1, short_w = w_tail && s == stages - 1;  // its missing pieces: any other one
-#pragma unroll
-        for (int i = 0; i < kXLoads; ++i)
-            load_to_lds(at + i * Shape::waves * 1024, short_x && x_piece[i] >= x_tail ? x_off[i] - x_piece[i] * 16 : x_off[i], x_base[i] + (int64_t)s * kXRow);
-#pragma unroll
-        for (int i = 0; i < kWLoads; ++i)
-            load_to_lds(at + kXBytes + i * Shape::waves * 1024, short_w && w_piece[i] >= w_tail ? w_off[i] - w_piece[i] * 16 : w_off[i],
-                        w_base + (int64_t)s * kWRow);
+        if (n < kXLoads) {
+            const bool missing = x_tail && s == stages - 1 && x_piece[n] >= x_tail;  // a piece behind the last input: any other one
+            load_to_lds(at + n * Shape::waves * 1024, missing ? x_off[n] - x_piece[n] * 16 : x_off[n], x_base[n] + (int64_t)s * kXRow);
+        } else {
+            const int i = n - kXLoads;
+            const bool missing = w_tail && s == stages - 1 && w_piece[i] >= w_tail;
+            load_to_lds(at + kXBytes + i * Shape::waves * 1024, missing ? w_off[i] - w_piece[i] * 16 : w_off[i], w_base + (int64_t)s * kWRow);
+        }
     };
 
-    // reads
+    // What a lane reads of a stage: 32 codes of every 16-row piece of x and of w, as they lie.  f of a lane's rows is the same for all
+    // pieces, so the pieces are constant offsets apart.
+    constexpr int kXWords = kXBits, kWWords = kWBits;
     const int x_row = wave_t * kP * 16 + r16, w_row = wave_n * 64 + 16 * (r16 >> 2) + (r16 & 3);
+    auto read_x = [&](int s, int i, int h, uint32_t (&v)[kXWords]) {  // 16 bytes
+        const uint4 q = *(const uint4 *)(tile_lds + (s & 1) * kStage + (x_row + i * 16) * kXRow +
+                                         (((kXBits == 8 ? 2 * g : g) + h) ^ x_turn<kXRow>(r16)) * 16);
+        v[4 * h] = q.x; v[4 * h + 1] = q.y; v[4 * h + 2] = q.z; v[4 * h + 3] = q.w;
+    };
+    auto read_w = [&](int s, int j, int h, uint32_t (&v)[4][kWWords]) {
+        const uint8_t *p = tile_lds + (s & 1) * kStage + kXBytes + (w_row + j * 4) * kWRow;
+        if constexpr (kWBits == 2) {
+            const uint2 q = *(const uint2 *)(p + ((g >> 1) ^ w_turn<kWRow>(w_row)) * 16 + (g & 1) * 8);
+            v[j][0] = q.x; v[j][1] = q.y;
+        } else {
+            const uint4 q = *(const uint4 *)(p + (((kWBits == 8 ? 2 * g : g) + h) ^ w_turn<kWRow>(w_row)) * 16);
+            v[j][4 * h] = q.x; v[j][4 * h + 1] = q.y; v[j][4 * h + 2] = q.z; v[j][4 * h + 3] = q.w;
+        }
+    };
+    // codes behind the last input count as 0 (then the weights' do not matter)
+    auto clear_tail = [&](int s) {
+        if (!x_tail || s != stages - 1) return;
+        for (int p = threadIdx.x; p < Shape::x_rows * (kXRow / 16); p += Shape::threads) {
+            const int row = p / (kXRow / 16), at = p % (kXRow / 16);
+            if ((at ^ x_turn<kXRow>(row)) >= x_tail) *(uint4 *)(tile_lds + (s & 1) * kStage + row * kXRow + at * 16) = make_uint4(0, 0, 0, 0);
+        }
+        __syncthreads();
+    };
+
+    // The reads run two pieces ahead of the products.  Once the last piece of a stage has been read, its LDS is free for the stage
+    // after the next; the products of the last two pieces cover the first reads of the next stage.  Reads and loads stand one by
+    // one between the products (four of them each), in the order written here: a wave issues in order, and in one burst behind the
+    // barrier the reads of 8 waves would hold up everyone's products.
+    constexpr int kRing = kP % 4 == 0 ? 4 : 3;
+    static_assert(kP % kRing == 0 && kP >= 4, "the ring's places are the same in every stage");
+    constexpr int kXReads = kXWords / 4, kWReads = kWBits == 8 ? 8 : 4;  // of a piece of x; of all of w
+    constexpr int kFirst = kWReads + 2 * kXReads;  // reads that a stage starts from
     i32x4 acc[kP][4] = {};
-    load_stage(0);
-    for (int s = 0; s < stages; ++s) {
-        // this wave's loads of stage s have landed, and with the barrier everyone's; everyone has read the other stage
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (s + 1 < stages) load_stage(s + 1);
-        uint8_t *xl = tile_lds + (s & 1) * kStage;
-        const uint8_t *wl = xl + kXBytes;
-        if (x_tail && s == stages - 1) {  // codes behind the last input count as 0 (then the weights' do not matter)
-            for (int p = threadIdx.x; p < Shape::x_rows * (kXRow / 16); p += Shape::threads) {
-                const int row = p / (kXRow / 16), at = p % (kXRow / 16);
-                if ((at ^ x_turn<kXRow>(row)) >= x_tail) *(uint4 *)(xl + row * kXRow + at * 16) = make_uint4(0, 0, 0, 0);
-            }
-            __syncthreads();
-        }
-        uint32_t wv[4][kWBits == 2 ? 2 : kWBits == 4 ? 4 : 8];
+    uint32_t wv[4][kWWords], xv[kRing][kXWords];
+    auto first_read = [&](int s, int n) {
+        // w's first halves, x's first piece, w's other halves, x's second piece
+        if (n < 4)
+            read_w(s, n, 0, wv);
+        else if (n < 4 + kXReads)
+            read_x(s, 0, n - 4, xv[0]);
+        else if (n < kWReads + kXReads)
+            read_w(s, n - 4 - kXReads, 1, wv);
+        else
+            read_x(s, 1, n - kWReads - kXReads, xv[1]);
+    };
+    auto stage = [&](int s, auto LEFT) {  // LEFT: stages behind this one, 2 for more
+        constexpr int left = decltype(LEFT)::value;
+        i32x4 a[2][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int row = w_row + 4 * j;
-            if constexpr (kWBits == 2) {
-                const uint2 v = *(const uint2 *)(wl + row * kWRow + ((g >> 1) ^ w_turn<kWRow>(row)) * 16 + (g & 1) * 8);
-                wv[j][0] = v.x; wv[j][1] = v.y;
-            } else {
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int h = 0; h < (kWBits == 8 ? 2 : 1); ++h) {
-                    const uint4 v = *(const uint4 *)(wl + row * kWRow + (((kWBits == 8 ? 2 * g : g) + h) ^ w_turn<kWRow>(row)) * 16);
-                    wv[j][4 * h] = v.x; wv[j][4 * h + 1] = v.y; wv[j][4 * h + 2] = v.z; wv[j][4 * h + 3] = v.w;
+            for (int j = 0; j < 4; ++j) a[h][j] = step_codes<kWBits, kNatural>(wv[j], h);
+        i32x4 b = step_codes<kXBits, kNatural>(xv[0], 0);
+#pragma unroll
+        for (int q = 0; q < 2 * kP; ++q) {
+            constexpr int kTurn = 2 * kP - 4;  // from here on the reads belong to the next stage
+            const int i = q >> 1, h = q & 1;
+            if (q < kTurn) {
+                if (h < kXReads) read_x(s, i + 2, h, xv[(i + 2) % kRing]);
+            } else if constexpr (left > 0) {
+                if (q == kTurn) {
+                    // this wave's loads of stage s + 1 have landed and its reads of stage s are done; with the barrier, everyone's
+                    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                    if (left == 1) clear_tail(s + 1);
                 }
-            }
-        }
+                if constexpr (left == 2) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            i32x4 a[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) a[j] = step_codes<kWBits, kNatural>(wv[j], h);
-#pragma unroll
-            for (int i = 0; i < kP; ++i) {
-                const int row = x_row + 16 * i;
-                i32x4 b;
-                if constexpr (kXBits == 8) {
-                    b = *(const i32x4 *)(xl + row * kXRow + ((2 * g + h) ^ x_turn<kXRow>(row)) * 16);
-                } else {
-                    const uint2 v = *(const uint2 *)(xl + row * kXRow + (g ^ x_turn<kXRow>(row)) * 16 + h * 8);
-                    const uint32_t q[2] = {v.x, v.y};
-                    b = step_codes<4, kNatural>(q, 0);
+                    for (int n = (q - kTurn) * kLoads / 4; n < (q - kTurn + 1) * kLoads / 4; ++n) load(s + 2, n);
                 }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[j], b, acc[i][j], 0, 0, 0);
+                for (int n = (q - kTurn) * kFirst / 4; n < (q - kTurn + 1) * kFirst / 4; ++n) first_read(s + 1, n);
             }
+            i32x4 next = b;
+            if (q + 1 < 2 * kP) next = step_codes<kXBits, kNatural>(xv[((q + 1) >> 1) % kRing], (q + 1) & 1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[h][j], b, acc[i][j], 0, 0, 0);
+            b = next;
+            __builtin_amdgcn_sched_barrier(0);
         }
+    };
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) load(0, n);
+    if (stages > 1) {
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) load(1, n);
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(kLoads) : "memory");
+    } else {
+        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        clear_tail(0);
     }
+#pragma unroll
+    for (int n = 0; n < kFirst; ++n) first_read(0, n);
+    for (int s = 0; s + 2 < stages; ++s) stage(s, std::integral_constant<int, 2>{});
+    if (stages > 1) stage(stages - 2, std::integral_constant<int, 1>{});
+    stage(stages - 1, std::integral_constant<int, 0>{});
 
     const int o = o0 + wave_n * 64 + g * 16;
     if (o >= A.n) return;
     float ws[16], bias[16];
+    int64_t channel[16];
 #pragma unroll
-    for (int c = 0; c < 16; ++c) {
-        const int64_t at = (int64_t)rt.expert * A.n + (o + c < A.n ? o + c : A.n - 1);
-        ws[c] = A.ws ? load_scale(A.ws, at, A.ws_f16) : 1.0f;
-        bias[c] = A.bias ? load_row_value(A.bias, at, A.dtype) : 0.0f;
-    }
+    for (int c = 0; c < 16; ++c) channel[c] = (int64_t)rt.expert * A.n + (o + c < A.n ? o + c : A.n - 1);
+    channel_scales(A, channel, ws);
+    channel_bias(A, channel, bias);
 #pragma unroll
     for (int i = 0; i < kP / kPlanes; ++i) {
         const int64_t t = rt.row0 + (wave_t * (kP / kPlanes) + i) * 16 + r16;

@@ -30,8 +30,8 @@ hipError_t launch_linear(const LinearArgs &A0, int xbits, int wbits, int planes,
         if (xbits == 8) return launch_linear_rows8(A, wbits, planes, blocks, stream);
         return launch_linear_rows4(A, wbits, blocks, stream);
     }
-    const int64_t tokens = planes == 1 ? 256 : planes == 2 ? 128 : 64;
-    const int64_t large_tiles = ((each + tokens - 1) / tokens) * A.experts * ((A.n + 255) / 256);
+    const int64_t tokens = planes == 1 ? 256 : 128, channels = planes == 3 ? 128 : 256;
+    const int64_t large_tiles = ((each + tokens - 1) / tokens) * A.experts * ((A.n + channels - 1) / channels);
     const bool large = large_tiles >= kCUs;
     if (planes > 1) return launch_linear_tile_digits(A, planes, large, stream);
     if (xbits == 8) return launch_linear_tile8(A, wbits, large, stream);

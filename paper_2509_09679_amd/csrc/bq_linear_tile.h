@@ -1,13 +1,13 @@
-// The product for many rows: a workgroup takes a tile of tokens x channels and walks along the sum's index 128 codes at a time, through
-// two stages in LDS.  The stages are filled by direct loads from memory (16 bytes per lane, no registers in between); one stage is
-// loaded while the other is multiplied.
+// The product for many rows: a workgroup takes a tile of tokens x channels and walks along the sum's index, 64 codes of 8 bits or 128
+// codes at a time, through a ring of stages in LDS.  The stages are filled by direct loads from memory (16 bytes per lane, no
+// registers in between); one stage is multiplied while the others are loaded.
 //
-// LDS rows are the codes of 128 inputs (128, 64 or 32 bytes), rows of x and of w after one another.  A direct load writes its 64
+// LDS rows are the codes of a stage (64 or 128 bytes of x or w, 64 or 32 of packed codes), rows of x and of w after one another.  A direct load writes its 64
 // lanes' pieces in lane order, so the order of a row's 16-byte pieces is made by which piece a lane loads: piece ^ f(row), with f such
 // that the 8 lanes of a 16-byte read that go together fall on different banks.
 //
-// A lane's 16 codes of the two matrix instructions of a stage are neighbours (32 g + 16 s .. of lane group g, step s): with packed codes
-// one read then serves both.  Row i of the first operand's piece j is channel 16 (i / 4) + 4 j + i % 4 of the wave's 64: a lane ends
+// Where a stage feeds two matrix instructions, a lane's 16 codes of the two are neighbours (32 g + 16 s .. of lane group g, step s):
+// with packed codes one read then serves both.  Row i of the first operand's piece j is channel 16 (i / 4) + 4 j + i % 4 of the wave's 64: a lane ends
 // with 16 consecutive channels of one token.
 #pragma once
 
@@ -23,6 +23,16 @@ struct TileShape {
     static constexpr int waves_t = kWavesT, waves_n = kWavesN, pieces = kPieces;
     static constexpr int waves = kWavesT * kWavesN, threads = 64 * waves;
     static constexpr int x_rows = kWavesT * kPieces * 16, w_rows = kWavesN * 64;
+};
+
+// The ring: matrix instructions along a stage's codes (64 each), bytes of a stage's rows, stages that fit.
+template <int kXBits, int kWBits, typename Shape>
+struct TileStages {
+    static constexpr int steps = 2;
+    static constexpr int x_row = steps * 8 * kXBits, w_row = steps * 8 * kWBits;
+    static constexpr int bytes = Shape::x_rows * x_row + Shape::w_rows * w_row;
+    static constexpr int fit = (Shape::waves == 8 ? 160 * 1024 : 80 * 1024) / bytes;
+    static constexpr int depth = fit < 4 ? fit : 4;
 };
 
 // f of the header comment.  A read of 16 bytes per lane goes 16 lanes at a time, {0-3, 12-15, 20-27} and {4-11, 16-19, 28-31} of either
@@ -48,7 +58,9 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, const
 template <int kXBits, int kWBits, int kPlanes, typename Shape>
 __global__ __launch_bounds__(Shape::threads, 1) void linear_tile_kernel(LinearArgs A)
 {
-    constexpr int kXRow = 16 * kXBits, kWRow = 16 * kWBits;  // bytes of 128 codes
+    typedef TileStages<kXBits, kWBits, Shape> Stages;
+    constexpr int kSteps = Stages::steps, kDepth = Stages::depth;
+    constexpr int kXRow = Stages::x_row, kWRow = Stages::w_row;
     constexpr int kXBytes = Shape::x_rows * kXRow, kWBytes = Shape::w_rows * kWRow, kStage = kXBytes + kWBytes;
     constexpr int kXLoads = kXBytes / 1024 / Shape::waves, kWLoads = kWBytes / 1024 / Shape::waves;
     static_assert(kXLoads * 1024 * Shape::waves == kXBytes && kWLoads * 1024 * Shape::waves == kWBytes, "whole loads per wave");
@@ -97,11 +109,11 @@ __global__ __launch_bounds__(Shape::threads, 1) void linear_tile_kernel(LinearAr
         w_piece[i] = (lane % (kWRow / 16)) ^ w_turn<kWRow>(row);
         w_off[i] = (uint32_t)(row < last ? row : last) * (uint32_t)A.ldw + w_piece[i] * 16;
     }
-    const int stages = (A.k + 127) / 128;
+    const int stages = (A.k + 64 * kSteps - 1) / (64 * kSteps);
     const int x_tail = (int)((int64_t)A.k * kXBits / 128) % (kXRow / 16), w_tail = (int)((int64_t)A.k * kWBits / 128) % (kWRow / 16);  // pieces of the last stage
     constexpr int kLoads = kXLoads + kWLoads;
-    auto load = [&](int s, int n) {  // the n-th of a stage's loads
-        const uint32_t at = lds0 + (s & 1) * kStage + wave * 1024;
+    auto load = [&](int s, int place, int n) {  // the n-th of stage s's loads, into a place of the ring
+        const uint32_t at = lds0 + place * kStage + wave * 1024;
         if (n < kXLoads) {
             const bool missing = x_tail && s == stages - 1 && x_piece[n] >= x_tail;  // a piece behind the last input: any other one
             load_to_lds(at + n * Shape::waves * 1024, missing ? x_off[n] - x_piece[n] * 16 : x_off[n], x_base[n] + (int64_t)s * kXRow);
@@ -112,106 +124,118 @@ __global__ __launch_bounds__(Shape::threads, 1) void linear_tile_kernel(LinearAr
         }
     };
 
-    // What a lane reads of a stage: 32 codes of every 16-row piece of x and of w, as they lie.  f of a lane's rows is the same for all
+    // What a lane reads of a stage: 16 or 32 codes of every 16-row piece of x and of w, as they lie.  f of a lane's rows is the same for all
     // pieces, so the pieces are constant offsets apart.
-    constexpr int kXWords = kXBits, kWWords = kWBits;
+    constexpr int kXWords = kXRow / 16, kWWords = kWRow / 16;
     const int x_row = wave_t * kP * 16 + r16, w_row = wave_n * 64 + 16 * (r16 >> 2) + (r16 & 3);
-    auto read_x = [&](int s, int i, int h, uint32_t (&v)[kXWords]) {  // 16 bytes
-        const uint4 q = *(const uint4 *)(tile_lds + (s & 1) * kStage + (x_row + i * 16) * kXRow +
-                                         (((kXBits == 8 ? 2 * g : g) + h) ^ x_turn<kXRow>(r16)) * 16);
+    auto read_x = [&](int place, int i, int h, uint32_t (&v)[kXWords]) {  // 16 bytes
+        const uint4 q = *(const uint4 *)(tile_lds + place * kStage + (x_row + i * 16) * kXRow +
+                                         (((kXWords == 8 ? 2 * g : g) + h) ^ x_turn<kXRow>(r16)) * 16);
         v[4 * h] = q.x; v[4 * h + 1] = q.y; v[4 * h + 2] = q.z; v[4 * h + 3] = q.w;
     };
-    auto read_w = [&](int s, int j, int h, uint32_t (&v)[4][kWWords]) {
-        const uint8_t *p = tile_lds + (s & 1) * kStage + kXBytes + (w_row + j * 4) * kWRow;
+    auto read_w = [&](int place, int j, int h, uint32_t (&v)[4][kWWords]) {
+        const uint8_t *p = tile_lds + place * kStage + kXBytes + (w_row + j * 4) * kWRow;
         if constexpr (kWBits == 2) {
             const uint2 q = *(const uint2 *)(p + ((g >> 1) ^ w_turn<kWRow>(w_row)) * 16 + (g & 1) * 8);
             v[j][0] = q.x; v[j][1] = q.y;
         } else {
-            const uint4 q = *(const uint4 *)(p + (((kWBits == 8 ? 2 * g : g) + h) ^ w_turn<kWRow>(w_row)) * 16);
+            const uint4 q = *(const uint4 *)(p + (((kWWords == 8 ? 2 * g : g) + h) ^ w_turn<kWRow>(w_row)) * 16);
             v[j][4 * h] = q.x; v[j][4 * h + 1] = q.y; v[j][4 * h + 2] = q.z; v[j][4 * h + 3] = q.w;
         }
     };
     // codes behind the last input count as 0 (then the weights' do not matter)
-    auto clear_tail = [&](int s) {
+    auto clear_tail = [&](int s, int place) {
         if (!x_tail || s != stages - 1) return;
         for (int p = threadIdx.x; p < Shape::x_rows * (kXRow / 16); p += Shape::threads) {
             const int row = p / (kXRow / 16), at = p % (kXRow / 16);
-            if ((at ^ x_turn<kXRow>(row)) >= x_tail) *(uint4 *)(tile_lds + (s & 1) * kStage + row * kXRow + at * 16) = make_uint4(0, 0, 0, 0);
+            if ((at ^ x_turn<kXRow>(row)) >= x_tail) *(uint4 *)(tile_lds + place * kStage + row * kXRow + at * 16) = make_uint4(0, 0, 0, 0);
         }
         __syncthreads();
     };
 
-    // The reads run two pieces ahead of the products.  Once the last piece of a stage has been read, its LDS is free for the stage
-    // after the next; the products of the last two pieces cover the first reads of the next stage.  Reads and loads stand one by
-    // one between the products (four of them each), in the order written here: a wave issues in order, and in one burst behind the
-    // barrier the reads of 8 waves would hold up everyone's products.
+    // The reads run two pieces ahead of the products.  Once the last piece of a stage has been read, its place is free for the stage
+    // kDepth further on; the products of the last two pieces cover the first reads of the next stage.  Reads and loads stand one
+    // by one between the products (four of them each), in the order written here: a wave issues in order, and in one burst behind
+    // the barrier the reads of 8 waves would hold up everyone's products.
     constexpr int kRing = kP % 4 == 0 ? 4 : 3;
     static_assert(kP % kRing == 0 && kP >= 4, "the ring's places are the same in every stage");
-    constexpr int kXReads = kXWords / 4, kWReads = kWBits == 8 ? 8 : 4;  // of a piece of x; of all of w
+    constexpr int kXReads = kXWords / 4, kWReads = kWWords == 8 ? 8 : 4;  // of a piece of x; of all of w
     constexpr int kFirst = kWReads + 2 * kXReads;  // reads that a stage starts from
     i32x4 acc[kP][4] = {};
     uint32_t wv[4][kWWords], xv[kRing][kXWords];
-    auto first_read = [&](int s, int n) {
+    auto first_read = [&](int place, int n) {
         // w's first halves, x's first piece, w's other halves, x's second piece
         if (n < 4)
-            read_w(s, n, 0, wv);
+            read_w(place, n, 0, wv);
         else if (n < 4 + kXReads)
-            read_x(s, 0, n - 4, xv[0]);
+            read_x(place, 0, n - 4, xv[0]);
         else if (n < kWReads + kXReads)
-            read_w(s, n - 4 - kXReads, 1, wv);
+            read_w(place, n - 4 - kXReads, 1, wv);
         else
-            read_x(s, 1, n - kWReads - kXReads, xv[1]);
+            read_x(place, 1, n - kWReads - kXReads, xv[1]);
     };
-    auto stage = [&](int s, auto LEFT) {  // LEFT: stages behind this one, 2 for more
+    auto stage = [&](int s, int place, int next_place, auto LEFT) {  // LEFT: 2 in the ring's steady state, 1 behind the last load, 0 the last
         constexpr int left = decltype(LEFT)::value;
-        i32x4 a[2][4];
+        i32x4 a[kSteps][4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < kSteps; ++h)
 #pragma unroll
             for (int j = 0; j < 4; ++j) a[h][j] = step_codes<kWBits, kNatural>(wv[j], h);
         i32x4 b = step_codes<kXBits, kNatural>(xv[0], 0);
 #pragma unroll
-        for (int q = 0; q < 2 * kP; ++q) {
-            constexpr int kTurn = 2 * kP - 4;  // from here on the reads belong to the next stage
-            const int i = q >> 1, h = q & 1;
+        for (int q = 0; q < kSteps * kP; ++q) {
+            constexpr int kOver = 2 * kSteps, kTurn = kSteps * kP - kOver;  // from here on the reads belong to the next stage
+            const int i = q / kSteps, h = q % kSteps;
             if (q < kTurn) {
-                if (h < kXReads) read_x(s, i + 2, h, xv[(i + 2) % kRing]);
+                if (h < kXReads) read_x(place, i + 2, h, xv[(i + 2) % kRing]);
             } else if constexpr (left > 0) {
                 if (q == kTurn) {
                     // this wave's loads of stage s + 1 have landed and its reads of stage s are done; with the barrier, everyone's
-                    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                    if (left == 1) clear_tail(s + 1);
+                    if constexpr (left == 2)
+                        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((kDepth - 2) * kLoads) : "memory");
+                    else
+                        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                    if (left == 1) clear_tail(s + 1, next_place);
                 }
                 if constexpr (left == 2) {
 #pragma unroll
-                    for (int n = (q - kTurn) * kLoads / 4; n < (q - kTurn + 1) * kLoads / 4; ++n) load(s + 2, n);
+                    for (int n = (q - kTurn) * kLoads / kOver; n < (q - kTurn + 1) * kLoads / kOver; ++n) load(s + kDepth, place, n);
                 }
 #pragma unroll
-                for (int n = (q - kTurn) * kFirst / 4; n < (q - kTurn + 1) * kFirst / 4; ++n) first_read(s + 1, n);
+                for (int n = (q - kTurn) * kFirst / kOver; n < (q - kTurn + 1) * kFirst / kOver; ++n) first_read(next_place, n);
             }
             i32x4 next = b;
-            if (q + 1 < 2 * kP) next = step_codes<kXBits, kNatural>(xv[((q + 1) >> 1) % kRing], (q + 1) & 1);
+            if (q + 1 < kSteps * kP) next = step_codes<kXBits, kNatural>(xv[((q + 1) / kSteps) % kRing], (q + 1) % kSteps);
 #pragma unroll
             for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[h][j], b, acc[i][j], 0, 0, 0);
             b = next;
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    static_assert((kDepth - 1) * kLoads < 64, "the wait's counter has 6 bits");
+    for (int s = 0; s < kDepth && s < stages; ++s) {
 #pragma unroll
-    for (int n = 0; n < kLoads; ++n) load(0, n);
-    if (stages > 1) {
-#pragma unroll
-        for (int n = 0; n < kLoads; ++n) load(1, n);
-        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(kLoads) : "memory");
-    } else {
-        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-        clear_tail(0);
+        for (int n = 0; n < kLoads; ++n) load(s, s, n);
     }
+    if (stages >= kDepth)
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((kDepth - 1) * kLoads) : "memory");
+    else
+        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    clear_tail(0, 0);
 #pragma unroll
     for (int n = 0; n < kFirst; ++n) first_read(0, n);
-    for (int s = 0; s + 2 < stages; ++s) stage(s, std::integral_constant<int, 2>{});
-    if (stages > 1) stage(stages - 2, std::integral_constant<int, 1>{});
-    stage(stages - 1, std::integral_constant<int, 0>{});
+    int s = 0, place = 0;
+    for (; s + kDepth < stages; ++s) {
+        const int next = place + 1 == kDepth ? 0 : place + 1;
+        stage(s, place, next, std::integral_constant<int, 2>{});
+        place = next;
+    }
+    for (; s + 1 < stages; ++s) {
+        const int next = place + 1 == kDepth ? 0 : place + 1;
+        stage(s, place, next, std::integral_constant<int, 1>{});
+        place = next;
+    }
+    stage(s, place, 0, std::integral_constant<int, 0>{});
 
     const int o = o0 + wave_n * 64 + g * 16;
     if (o >= A.n) return;
@@ -243,7 +267,7 @@ __global__ __launch_bounds__(Shape::threads, 1) void linear_tile_kernel(LinearAr
 template <int kXBits, int kWBits, int kPlanes, typename Shape>
 hipError_t launch_tile(const LinearArgs &A, hipStream_t stream)
 {
-    constexpr size_t kLds = 2 * (size_t)(Shape::x_rows * 16 * kXBits + Shape::w_rows * 16 * kWBits);
+    constexpr size_t kLds = (size_t)TileStages<kXBits, kWBits, Shape>::depth * TileStages<kXBits, kWBits, Shape>::bytes;
     static LdsLimitOnce limit;
     const hipError_t e = limit.set((const void *)linear_tile_kernel<kXBits, kWBits, kPlanes, Shape>, kLds);
     if (e != hipSuccess) return e;
@@ -255,7 +279,7 @@ hipError_t launch_tile(const LinearArgs &A, hipStream_t stream)
 }
 
 typedef TileShape<2, 4, 8> TileLarge;   // 256 tokens x 256 channels, or 128 x 256 of two planes
-typedef TileShape<2, 4, 6> TileLarge3;  // 64 tokens of three planes x 256
+typedef TileShape<4, 2, 6> TileLarge3;  // 128 tokens of three planes x 128
 typedef TileShape<2, 2, 4> TileSmall;   // 128 x 128, or 64 x 128 of two planes
 typedef TileShape<2, 2, 6> TileSmall3;  // 64 tokens of three planes x 128
 

@@ -20,7 +20,7 @@ bool fast_layout(const LinearArgs &A, int xbits, int wbits)
 hipError_t launch_linear(const LinearArgs &A0, int xbits, int wbits, int planes, hipStream_t stream)
 {
     LinearArgs A = A0;
-    A.factor = 1.0f / (float)((1 << (8 - xbits)) * (1 << (8 - wbits)));
+    A.factor /= (float)((1 << (8 - xbits)) * (1 << (8 - wbits)));
     const size_t size = A.dtype == BQ_F32 ? 4 : 2;
     A.y_quads = (uintptr_t)A.y % 16 == 0 && A.ldy * size % 16 == 0;
     if (!fast_layout(A, xbits, wbits)) return launch_linear_any(A, xbits, wbits, planes, stream);

@@ -7,7 +7,7 @@
 // would leave.  Digits cost the matrix cores less than they look: two products of 8 bits take the time of one of 16 bits.  A row
 // with an infinity or NaN gets f = NaN: its gradient is NaN throughout.
 #include "bq_cascade.h"
-#include "bq_linear.h"
+#include "bq_linear_codes.h"
 
 namespace bq {
 
@@ -52,66 +52,131 @@ __device__ __forceinline__ int expert_of(const int32_t *offsets, int experts, in
     return -1;
 }
 
-template <typename T, int kPlanes>
-__global__ __launch_bounds__(256) void linear_digits_kernel(DigitArgs A, int vec)
+// the factor of a row and what its entries are multiplied with, from the bit pattern of its largest magnitude
+struct RowFactor {
+    float lift, inv, factor;
+};
+
+template <int kPlanes>
+__device__ __forceinline__ RowFactor row_factor(uint32_t amax_bits)
 {
     constexpr float kMost = kPlanes == 3 ? 8355711.0f : 32639.0f;
-    for (int64_t row = blockIdx.x; row < A.rows; row += gridDim.x) {
-        const int expert = expert_of(A.offsets, A.experts, row);
-        if (expert < 0) continue;  // (the product does not look at it)
-        const T *dy = (const T *)A.dy + row * A.ld_dy;
-        const int64_t s0 = (int64_t)expert * A.n;
-        auto eight = [&](int c, float (&v)[8]) {  // dy ws of 8 channels, 0 behind the last
-            if (vec && c + 8 <= A.n) {
-                unpack8(load8(dy + c), v, (const T *)nullptr);
+    const bool finite = amax_bits < 0x7F800000u;
+    const float amax = __uint_as_float(amax_bits);
+    // rows of tiny entries are lifted first: m / amax has to be a float32 number
+    RowFactor f;
+    f.lift = amax < 0x1p-60f ? 0x1p60f : 1.0f;
+    const float top = amax * f.lift;
+    const bool some = finite && top >= 0x1p-60f;  // (below 2^-120 the row counts as 0)
+    f.inv = some ? kMost / top : 0.0f;
+    f.factor = !finite ? __uint_as_float(0x7FC00000u) : some ? (top / kMost) / f.lift : 0.0f;
+    return f;
+}
+
+// the digits of 8 entries, packed by plane
+template <int kPlanes>
+__device__ __forceinline__ void digits8(const float (&v)[8], const RowFactor &f, uint2 (&d)[kPlanes])
+{
+    constexpr float kMost = kPlanes == 3 ? 8355711.0f : 32639.0f;
+    uint32_t w[kPlanes][2] = {};
 #pragma unroll
-                for (int r = 0; r < 8; ++r) v[r] *= load_scale(A.ws, s0 + c + r, A.ws_f16);
-            } else {
+    for (int r = 0; r < 8; ++r) {
+        const float q = rintf(v[r] * f.lift * f.inv);
+        const int u = f.inv == 0.0f ? 0 : (int)fminf(fmaxf(q, -kMost), kMost);
+        const int low = (u + 128) >> 8;  // u without its lowest digit, over 256
+        const int sh = (r & 3) * 8;
+        w[kPlanes - 1][r >> 2] |= ((uint32_t)u & 255u) << sh;  // (the digits modulo 256 are the bytes)
+        if (kPlanes == 3) {
+            w[kPlanes - 2][r >> 2] |= ((uint32_t)low & 255u) << sh;
+            w[0][r >> 2] |= ((uint32_t)((low + 128) >> 8) & 255u) << sh;
+        } else {
+            w[0][r >> 2] |= ((uint32_t)low & 255u) << sh;
+        }
+    }
 #pragma unroll
-                for (int r = 0; r < 8; ++r) v[r] = c + r < A.n ? to_float(dy[c + r]) * load_scale(A.ws, s0 + c + r, A.ws_f16) : 0.0f;
+    for (int p = 0; p < kPlanes; ++p) d[p] = make_uint2(w[p][0], w[p][1]);
+}
+
+// Rows of whole, aligned pieces of 8: a workgroup takes neighbouring rows, which mostly belong to one expert, and keeps that expert's
+// scales and a row's products in registers; kPasses pieces per thread.  One read of dy and one write of the digits: bound by HBM.
+template <typename T, int kPlanes, int kPasses>
+__global__ __launch_bounds__(256) void linear_digits_kernel(DigitArgs A, int rows_each)
+{
+    const int64_t first = (int64_t)blockIdx.x * rows_each;
+    const int64_t end = first + rows_each < A.rows ? first + rows_each : A.rows;
+    float ws[kPasses][8];
+    int expert = -1;
+    for (int64_t row = first; row < end; ++row) {
+        const int e = expert_of(A.offsets, A.experts, row);
+        if (e < 0) continue;  // (the product does not look at it)
+        if (e != expert) {
+            expert = e;
+#pragma unroll
+            for (int p = 0; p < kPasses; ++p) {
+                const int c = (p * 256 + threadIdx.x) * 8;
+                const int64_t at = (int64_t)e * A.n + (c < A.n ? c : 0);
+                if (A.ws_f16)
+                    unpack8(load8((const __half *)A.ws + at), ws[p], (const __half *)nullptr);
+                else
+                    unpack8(load8((const float *)A.ws + at), ws[p], (const float *)nullptr);
             }
-        };
+        }
+        const T *dy = (const T *)A.dy + row * A.ld_dy;
+        float v[kPasses][8];
         uint32_t m = 0;
-        for (int c = threadIdx.x * 8; c < A.n; c += 2048) {
-            float v[8];
-            eight(c, v);
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) {
+            const int c = (p * 256 + threadIdx.x) * 8;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) v[p][r] = 0.0f;
+            if (c >= A.n) continue;
+            unpack8(load8(dy + c), v[p], (const T *)nullptr);
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
-                const uint32_t b = __float_as_uint(v[r]) & 0x7FFFFFFFu;
+                v[p][r] *= ws[p][r];
+                const uint32_t b = __float_as_uint(v[p][r]) & 0x7FFFFFFFu;
                 m = m > b ? m : b;
             }
         }
-        m = block_max(m);
-        const bool finite = m < 0x7F800000u;
-        const float amax = __uint_as_float(m);
-        // rows of tiny entries are lifted first: m / amax has to be a float32 number
-        const float lift = amax < 0x1p-60f ? 0x1p60f : 1.0f;
-        const float top = amax * lift;
-        const bool some = finite && top >= 0x1p-60f;  // (below 2^-120 the row counts as 0)
-        const float inv = some ? kMost / top : 0.0f;
-        if (threadIdx.x == 0) A.factor[row] = !finite ? __uint_as_float(0x7FC00000u) : some ? (top / kMost) / lift : 0.0f;
+        const RowFactor f = row_factor<kPlanes>(block_max(m));
+        if (threadIdx.x == 0) A.factor[row] = f.factor;
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) {
+            const int c = (p * 256 + threadIdx.x) * 8;
+            if (c >= A.np) continue;
+            uint2 d[kPlanes];
+            digits8<kPlanes>(v[p], f, d);
+#pragma unroll
+            for (int q = 0; q < kPlanes; ++q) *(uint2 *)(A.planes + ((int64_t)q * A.rows + row) * A.np + c) = d[q];
+        }
+    }
+}
+
+// Any rows; the second look at a row comes from the caches.
+template <typename T, int kPlanes>
+__global__ __launch_bounds__(256) void linear_digits_any_kernel(DigitArgs A)
+{
+    for (int64_t row = blockIdx.x; row < A.rows; row += gridDim.x) {
+        const int expert = expert_of(A.offsets, A.experts, row);
+        if (expert < 0) continue;
+        const T *dy = (const T *)A.dy + row * A.ld_dy;
+        const int64_t s0 = (int64_t)expert * A.n;
+        auto entry = [&](int c) { return c < A.n ? to_float(dy[c]) * load_scale(A.ws, s0 + c, A.ws_f16) : 0.0f; };
+        uint32_t m = 0;
+        for (int c = threadIdx.x; c < A.n; c += 256) {
+            const uint32_t b = __float_as_uint(entry(c)) & 0x7FFFFFFFu;
+            m = m > b ? m : b;
+        }
+        const RowFactor f = row_factor<kPlanes>(block_max(m));
+        if (threadIdx.x == 0) A.factor[row] = f.factor;
         for (int c = threadIdx.x * 8; c < A.np; c += 2048) {
             float v[8];
-            eight(c, v);
-            uint32_t d[kPlanes][2] = {};
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                const float q = rintf(v[r] * lift * inv);
-                const int u = some ? (int)fminf(fmaxf(q, -kMost), kMost) : 0;
-                const int low = (u + 128) >> 8;  // u without its lowest digit, over 256
-                const int sh = (r & 3) * 8;
-                d[kPlanes - 1][r >> 2] |= ((uint32_t)(u - low * 256) & 255u) << sh;
-                if (kPlanes == 3) {
-                    const int high = (low + 128) >> 8;
-                    d[kPlanes - 2][r >> 2] |= ((uint32_t)(low - high * 256) & 255u) << sh;
-                    d[0][r >> 2] |= ((uint32_t)high & 255u) << sh;
-                } else {
-                    d[0][r >> 2] |= ((uint32_t)low & 255u) << sh;
-                }
-            }
+            for (int r = 0; r < 8; ++r) v[r] = entry(c + r);
+            uint2 d[kPlanes];
+            digits8<kPlanes>(v, f, d);
 #pragma unroll
-            for (int p = 0; p < kPlanes; ++p)
-                *(uint2 *)(A.planes + ((int64_t)p * A.rows + row) * A.np + c) = make_uint2(d[p][0], d[p][1]);
+            for (int q = 0; q < kPlanes; ++q) *(uint2 *)(A.planes + ((int64_t)q * A.rows + row) * A.np + c) = d[q];
         }
     }
 }
@@ -121,57 +186,82 @@ struct TransposeArgs {
     int8_t *out;  // [experts][k][np]
     const int32_t *offsets;
     int64_t ldw, w_step;
-    int n, k, np, bits, vec;
+    int n, k, np;
 };
 
-constexpr int kTr = 64;
+__device__ __forceinline__ bool has_rows(const int32_t *offsets, int expert) { return !offsets || offsets[expert] < offsets[expert + 1]; }
 
-// 64 outputs x 64 inputs per workgroup through LDS; codes of 4 and 2 bits come out as whole bytes.
+constexpr int kTr = 128;
+
+// 128 outputs x 128 inputs per workgroup.  A thread reads 16 codes of four neighbouring outputs, turns them in registers, 4 x 4 bytes at
+// a time, and stores words of four outputs to LDS, from where the result's rows leave in whole lines.  Codes of 4 and 2 bits come
+// out as bytes with the code at the top, 16 or 64 times its value.  One read of w, one write: bound by HBM.
+template <int kBits>
 __global__ __launch_bounds__(256) void linear_transpose_kernel(TransposeArgs A)
 {
-    __shared__ __align__(16) uint8_t s[kTr][kTr + 4];
+    constexpr int kLd = kTr / 4 + 1;
+    __shared__ uint32_t s[kTr * kLd];
     const int expert = blockIdx.z;
-    if (A.offsets && A.offsets[expert + 1] <= A.offsets[expert]) return;  // no rows
+    if (!has_rows(A.offsets, expert)) return;
     const int k0 = blockIdx.x * kTr, o0 = blockIdx.y * kTr;
-    const int row = threadIdx.x >> 2, part = (threadIdx.x & 3) * 16;
-    const uint8_t *w = A.w + expert * A.w_step + (int64_t)(o0 + row) * A.ldw;
-    uint32_t c[4] = {};
-    if (o0 + row < A.n) {
-        if (A.vec && k0 + part + 16 <= A.k) {
-            if (A.bits == 8) {
-                const uint4 v = *(const uint4 *)(w + k0 + part);
-                c[0] = v.x; c[1] = v.y; c[2] = v.z; c[3] = v.w;
-            } else {
-                const int per = 8 / A.bits;
-                const uint8_t *p = w + (k0 + part) / per;
+    const int quad = threadIdx.x >> 3, part = (threadIdx.x & 7) * 16;
+    uint32_t c[4][4] = {};  // [output][word]
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int f = (int)(int8_t)(uint8_t)(p[j / per] << (8 - A.bits - (j % per) * A.bits)) >> (8 - A.bits);
-                    c[j >> 2] |= ((uint32_t)f & 255u) << ((j & 3) * 8);
-                }
-            }
+    for (int r = 0; r < 4; ++r) {
+        const int o = o0 + quad * 4 + r;
+        if (o >= A.n || k0 + part >= A.k) continue;
+        const uint8_t *p = A.w + expert * A.w_step + (int64_t)o * A.ldw + (int64_t)(k0 + part) * kBits / 8;
+        if constexpr (kBits == 8) {
+            const uint4 v = *(const uint4 *)p;
+            c[r][0] = v.x; c[r][1] = v.y; c[r][2] = v.z; c[r][3] = v.w;
         } else {
+            uint32_t raw[kBits / 2];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const int k = k0 + part + j;
-                if (k >= A.k) continue;
-                const int per = 8 / A.bits;
-                const int f = (int)(int8_t)(uint8_t)(w[k / per] << (8 - A.bits - (k % per) * A.bits)) >> (8 - A.bits);
-                c[j >> 2] |= ((uint32_t)f & 255u) << ((j & 3) * 8);
-            }
+            for (int j = 0; j < kBits / 2; ++j) raw[j] = ((const uint32_t *)p)[j];
+            const i32x4 v = step_codes<kBits, true>(raw, 0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) c[r][j] = (uint32_t)v[j];
         }
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) *(uint32_t *)&s[row][part + 4 * j] = c[j];
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t t0 = __builtin_amdgcn_perm(c[1][j], c[0][j], 0x05010400u), t1 = __builtin_amdgcn_perm(c[1][j], c[0][j], 0x07030602u);
+        const uint32_t u0 = __builtin_amdgcn_perm(c[3][j], c[2][j], 0x05010400u), u1 = __builtin_amdgcn_perm(c[3][j], c[2][j], 0x07030602u);
+        uint32_t *q = s + (part + 4 * j) * kLd + quad;
+        q[0] = __builtin_amdgcn_perm(u0, t0, 0x05040100u);
+        q[kLd] = __builtin_amdgcn_perm(u0, t0, 0x07060302u);
+        q[2 * kLd] = __builtin_amdgcn_perm(u1, t1, 0x05040100u);
+        q[3 * kLd] = __builtin_amdgcn_perm(u1, t1, 0x07060302u);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = i * 32 + quad, k = k0 + row;
+        if (k >= A.k) continue;
+        const uint32_t *q = s + row * kLd + part / 4;
+        *(uint4 *)(A.out + ((int64_t)expert * A.k + k) * A.np + o0 + part) = make_uint4(q[0], q[1], q[2], q[3]);
+    }
+}
+
+// The same for any width and alignment, 64 x 64 codes one by one.
+__global__ __launch_bounds__(256) void linear_transpose_any_kernel(TransposeArgs A, int bits)
+{
+    __shared__ __align__(16) uint8_t s[64][64 + 4];
+    const int expert = blockIdx.z;
+    if (!has_rows(A.offsets, expert)) return;
+    const int k0 = blockIdx.x * 64, o0 = blockIdx.y * 64, per = 8 / bits;
+    const int row = threadIdx.x >> 2, part = (threadIdx.x & 3) * 16;
+    const uint8_t *w = A.w + expert * A.w_step + (int64_t)(o0 + row) * A.ldw;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        const int k = k0 + part + j;
+        s[row][part + j] = o0 + row < A.n && k < A.k ? (uint8_t)(w[k / per] << (8 - bits - (k % per) * bits)) & (0xFF00u >> bits) : 0;
+    }
     __syncthreads();
     const int k = k0 + row;  // now a row of the result
     if (k >= A.k) return;
-    uint32_t r[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        r[j] = (uint32_t)s[part + 4 * j][row] | (uint32_t)s[part + 4 * j + 1][row] << 8 | (uint32_t)s[part + 4 * j + 2][row] << 16 |
-               (uint32_t)s[part + 4 * j + 3][row] << 24;
-    *(uint4 *)(A.out + ((int64_t)expert * A.k + k) * A.np + o0 + part) = make_uint4(r[0], r[1], r[2], r[3]);
+    for (int j = 0; j < 16; ++j) A.out[((int64_t)expert * A.k + k) * A.np + o0 + part + j] = (int8_t)s[part + j][row];
 }
 
 int padded(int n) { return (n + 127) / 128 * 128; }
@@ -179,8 +269,39 @@ int padded(int n) { return (n + 127) / 128 * 128; }
 template <typename T, int kPlanes>
 hipError_t launch_digits(const DigitArgs &D, hipStream_t stream)
 {
-    const int vec = (uintptr_t)D.dy % 16 == 0 && D.ld_dy * sizeof(T) % 16 == 0;
-    hipLaunchKernelGGL((linear_digits_kernel<T, kPlanes>), dim3((unsigned)(D.rows < 65536 ? D.rows : 65536)), dim3(256), 0, stream, D, vec);
+    const bool vec = (uintptr_t)D.dy % 16 == 0 && D.ld_dy * sizeof(T) % 16 == 0 && D.n % 8 == 0 && (uintptr_t)D.ws % 16 == 0 && D.np <= 16384;
+    if (!vec) {
+        hipLaunchKernelGGL((linear_digits_any_kernel<T, kPlanes>), dim3((unsigned)(D.rows < 65536 ? D.rows : 65536)), dim3(256), 0, stream, D);
+        return hipGetLastError();
+    }
+    // 8 workgroups fit a compute unit; beyond 4096 they take several rows each
+    const int rows_each = (int)((D.rows + 4095) / 4096);
+    const dim3 grid((unsigned)((D.rows + rows_each - 1) / rows_each));
+    if (D.np <= 2048)
+        hipLaunchKernelGGL((linear_digits_kernel<T, kPlanes, 1>), grid, dim3(256), 0, stream, D, rows_each);
+    else if (D.np <= 4096)
+        hipLaunchKernelGGL((linear_digits_kernel<T, kPlanes, 2>), grid, dim3(256), 0, stream, D, rows_each);
+    else if (D.np <= 8192)
+        hipLaunchKernelGGL((linear_digits_kernel<T, kPlanes, 4>), grid, dim3(256), 0, stream, D, rows_each);
+    else
+        hipLaunchKernelGGL((linear_digits_kernel<T, kPlanes, 8>), grid, dim3(256), 0, stream, D, rows_each);
+    return hipGetLastError();
+}
+
+hipError_t launch_transpose(const TransposeArgs &R, int bits, int experts, hipStream_t stream)
+{
+    if (R.k % 16 == 0 && (uintptr_t)R.w % (2 * bits) == 0 && R.ldw % (2 * bits) == 0) {
+        const dim3 grid((unsigned)((R.k + kTr - 1) / kTr), (unsigned)(R.np / kTr), (unsigned)experts);
+        if (bits == 8)
+            hipLaunchKernelGGL(linear_transpose_kernel<8>, grid, dim3(256), 0, stream, R);
+        else if (bits == 4)
+            hipLaunchKernelGGL(linear_transpose_kernel<4>, grid, dim3(256), 0, stream, R);
+        else
+            hipLaunchKernelGGL(linear_transpose_kernel<2>, grid, dim3(256), 0, stream, R);
+        return hipGetLastError();
+    }
+    const dim3 grid((unsigned)((R.k + 63) / 64), (unsigned)(R.np / 64), (unsigned)experts);
+    hipLaunchKernelGGL(linear_transpose_any_kernel, grid, dim3(256), 0, stream, R, bits);
     return hipGetLastError();
 }
 
@@ -231,11 +352,7 @@ hipError_t launch_linear_bwd(const void *dy, int64_t ld_dy, const void *w, int w
     R.n = n;
     R.k = k;
     R.np = np;
-    R.bits = wbits;
-    R.vec = (uintptr_t)w % 16 == 0 && ldw % 16 == 0;
-    hipLaunchKernelGGL(linear_transpose_kernel, dim3((unsigned)((k + kTr - 1) / kTr), (unsigned)(np / kTr), (unsigned)experts), dim3(256), 0,
-                       stream, R);
-    e = hipGetLastError();
+    e = launch_transpose(R, wbits, experts, stream);
     if (e != hipSuccess) return e;
     LinearArgs A{};
     A.x = (const uint8_t *)(base + L.planes);
@@ -252,7 +369,7 @@ hipError_t launch_linear_bwd(const void *dy, int64_t ld_dy, const void *w, int w
     A.n = k;
     A.experts = experts;
     A.dtype = dtype;
-    A.factor = 1.0f;
+    A.factor = 1.0f / (float)(1 << (8 - wbits));
     return launch_linear(A, 8, 8, planes, stream);
 }
 

@@ -147,13 +147,14 @@ __device__ __forceinline__ void store_row_value(void *p, int64_t at, int dtype, 
 // ---- launchers --------------------------------------------------------------------------------------------
 hipError_t launch_linear_any(const LinearArgs &A, int xbits, int wbits, int planes, hipStream_t stream);  // bq_linear_any.hip
 int64_t linear_any_blocks(const LinearArgs &A);
-// few rows: bq_linear_rows.h; blocks: 16-token blocks of a pass, 1, 2 or 4
-hipError_t launch_linear_rows8(const LinearArgs &A, int wbits, int planes, int blocks, hipStream_t stream);
-hipError_t launch_linear_rows4(const LinearArgs &A, int wbits, int blocks, hipStream_t stream);
+// few rows: bq_linear_rows.h; blocks x cols: 16-token blocks and 16-channel columns of a workgroup
+hipError_t launch_linear_rows8(const LinearArgs &A, int wbits, int planes, int blocks, int cols, hipStream_t stream);
+hipError_t launch_linear_rows4(const LinearArgs &A, int wbits, int blocks, int cols, hipStream_t stream);
 // many: bq_linear_tile.h
-hipError_t launch_linear_tile8(const LinearArgs &A, int wbits, bool large, hipStream_t stream);
-hipError_t launch_linear_tile4(const LinearArgs &A, int wbits, bool large, hipStream_t stream);
-hipError_t launch_linear_tile_digits(const LinearArgs &A, int planes, bool large, hipStream_t stream);
+enum LinearTile { kTileLarge, kTileMiddle, kTileSmall, kTileDeep };
+hipError_t launch_linear_tile8(const LinearArgs &A, int wbits, LinearTile tile, hipStream_t stream);
+hipError_t launch_linear_tile4(const LinearArgs &A, int wbits, LinearTile tile, hipStream_t stream);
+hipError_t launch_linear_tile_digits(const LinearArgs &A, int planes, LinearTile tile, hipStream_t stream);
 // picks the kernel; planes: 1 for codes, 2 or 3 for a gradient's digits (bq_linear.hip)
 hipError_t launch_linear(const LinearArgs &A, int xbits, int wbits, int planes, hipStream_t stream);
 

@@ -66,19 +66,31 @@ __device__ __forceinline__ float joined(const int (&sum)[kPlanes])
     if constexpr (kPlanes == 3) return (float)__builtin_fma((double)sum[0], 65536.0, __builtin_fma((double)sum[1], 256.0, (double)sum[2]));
 }
 
-// scales and bias of some channels: every type's loads in a branch of its own, so that they are in flight together
+// scales and bias of some channels or tokens: every type's loads in a branch of its own, so that they are in flight together
+template <int kCount>
+__device__ __forceinline__ void load_scales(const void *p, int f16, const int64_t (&at)[kCount], float (&s)[kCount])
+{
+    if (f16) {
+#pragma unroll
+        for (int c = 0; c < kCount; ++c) s[c] = __half2float(((const __half *)p)[at[c]]);
+    } else {
+#pragma unroll
+        for (int c = 0; c < kCount; ++c) s[c] = ((const float *)p)[at[c]];
+    }
+}
+template <int kCount>
+__device__ __forceinline__ void token_scales(const LinearArgs &A, const int64_t (&at)[kCount], float (&s)[kCount])
+{
+    load_scales(A.xs, A.xs_f16, at, s);
+}
 template <int kCount>
 __device__ __forceinline__ void channel_scales(const LinearArgs &A, const int64_t (&at)[kCount], float (&s)[kCount])
 {
-    if (!A.ws) {
-#pragma unroll
-        for (int c = 0; c < kCount; ++c) s[c] = 1.0f;
-    } else if (A.ws_f16) {
-#pragma unroll
-        for (int c = 0; c < kCount; ++c) s[c] = __half2float(((const __half *)A.ws)[at[c]]);
+    if (A.ws) {
+        load_scales(A.ws, A.ws_f16, at, s);
     } else {
 #pragma unroll
-        for (int c = 0; c < kCount; ++c) s[c] = ((const float *)A.ws)[at[c]];
+        for (int c = 0; c < kCount; ++c) s[c] = 1.0f;
     }
 }
 template <int kCount>

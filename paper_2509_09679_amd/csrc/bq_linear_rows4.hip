@@ -3,11 +3,11 @@
 
 namespace bq {
 
-hipError_t launch_linear_rows4(const LinearArgs &A, int wbits, int blocks, hipStream_t stream)
+hipError_t launch_linear_rows4(const LinearArgs &A, int wbits, int blocks, int cols, hipStream_t stream)
 {
-    if (wbits == 8) return launch_rows<4, 8, 1>(A, blocks, stream);
-    if (wbits == 4) return launch_rows<4, 4, 1>(A, blocks, stream);
-    return launch_rows<4, 2, 1>(A, blocks, stream);
+    if (wbits == 8) return launch_rows_of<4, 8, 1>(A, blocks, cols, stream);
+    if (wbits == 4) return launch_rows_of<4, 4, 1>(A, blocks, cols, stream);
+    return launch_rows_of<4, 2, 1>(A, blocks, cols, stream);
 }
 
 }  // namespace bq

@@ -18,12 +18,16 @@
 namespace bq {
 
 // Waves of a workgroup along tokens and channels, 16-row pieces of a wave along tokens (of x's rows: planes count); 64 channels per wave.
-template <int kWavesT, int kWavesN, int kPieces>
+// kLds: what the ring may take of a compute unit's LDS, in KB.
+template <int kWavesT, int kWavesN, int kPieces, int kLds>
 struct TileShape {
+    static constexpr int lds = kLds * 1024;
     static constexpr int waves_t = kWavesT, waves_n = kWavesN, pieces = kPieces;
     static constexpr int waves = kWavesT * kWavesN, threads = 64 * waves;
     static constexpr int x_rows = kWavesT * kPieces * 16, w_rows = kWavesN * 64;
 };
+
+constexpr int kMostStages = 4;
 
 // The ring: matrix instructions along a stage's codes (64 each), bytes of a stage's rows, stages that fit.
 template <int kXBits, int kWBits, typename Shape>
@@ -31,8 +35,8 @@ struct TileStages {
     static constexpr int steps = 2;
     static constexpr int x_row = steps * 8 * kXBits, w_row = steps * 8 * kWBits;
     static constexpr int bytes = Shape::x_rows * x_row + Shape::w_rows * w_row;
-    static constexpr int fit = (Shape::waves == 8 ? 160 * 1024 : 80 * 1024) / bytes;
-    static constexpr int depth = fit < 4 ? fit : 4;
+    static constexpr int fit = Shape::lds / bytes;
+    static constexpr int depth = fit < kMostStages ? fit : kMostStages;
 };
 
 // f of the header comment.  A read of 16 bytes per lane goes 16 lanes at a time, {0-3, 12-15, 20-27} and {4-11, 16-19, 28-31} of either
@@ -56,7 +60,7 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, const
 }
 
 template <int kXBits, int kWBits, int kPlanes, typename Shape>
-__global__ __launch_bounds__(Shape::threads, 1) void linear_tile_kernel(LinearArgs A)
+__global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearArgs A)
 {
     typedef TileStages<kXBits, kWBits, Shape> Stages;
     constexpr int kSteps = Stages::steps, kDepth = Stages::depth;
@@ -162,8 +166,8 @@ __global__ __launch_bounds__(Shape::threads, 1) void linear_tile_kernel(LinearAr
     constexpr int kXReads = kXWords / 4, kWReads = kWWords == 8 ? 8 : 4;  // of a piece of x; of all of w
     constexpr int kFirst = kWReads + 2 * kXReads;  // reads that a stage starts from
     i32x4 acc[kP][4] = {};
-    uint32_t wv[4][kWWords], xv[kRing][kXWords];
-    auto first_read = [&](int place, int n) {
+    uint32_t wv[2][4][kWWords], xv[kRing][kXWords];  // (w's codes alternate: in one array every stage began by copying them)
+    auto first_read = [&](int place, int n, uint32_t (&wv)[4][kWWords]) {
         // w's first halves, x's first piece, w's other halves, x's second piece
         if (n < 4)
             read_w(place, n, 0, wv);
@@ -174,7 +178,7 @@ __global__ __launch_bounds__(Shape::threads, 1) void linear_tile_kernel(LinearAr
         else
             read_x(place, 1, n - kWReads - kXReads, xv[1]);
     };
-    auto stage = [&](int s, int place, int next_place, auto LEFT) {  // LEFT: 2 in the ring's steady state, 1 behind the last load, 0 the last
+    auto stage = [&](int s, int place, int next_place, const uint32_t (&wv)[4][kWWords], uint32_t (&wn)[4][kWWords], auto LEFT) {  // LEFT: 2 in the ring's steady state, 1 behind the last load, 0 the last
         constexpr int left = decltype(LEFT)::value;
         i32x4 a[kSteps][4];
 #pragma unroll
@@ -202,7 +206,7 @@ __global__ __launch_bounds__(Shape::threads, 1) void linear_tile_kernel(LinearAr
                     for (int n = (q - kTurn) * kLoads / kOver; n < (q - kTurn + 1) * kLoads / kOver; ++n) load(s + kDepth, place, n);
                 }
 #pragma unroll
-                for (int n = (q - kTurn) * kFirst / kOver; n < (q - kTurn + 1) * kFirst / kOver; ++n) first_read(next_place, n);
+                for (int n = (q - kTurn) * kFirst / kOver; n < (q - kTurn + 1) * kFirst / kOver; ++n) first_read(next_place, n, wn);
             }
             i32x4 next = b;
             if (q + 1 < kSteps * kP) next = step_codes<kXBits, kNatural>(xv[((q + 1) / kSteps) % kRing], (q + 1) % kSteps);
@@ -212,7 +216,7 @@ __global__ __launch_bounds__(Shape::threads, 1) void linear_tile_kernel(LinearAr
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    static_assert((kDepth - 1) * kLoads < 64, "the wait's counter has 6 bits");
+    static_assert(kDepth >= 2 && (kDepth - 1) * kLoads < 64, "the wait's counter has 6 bits");
     for (int s = 0; s < kDepth && s < stages; ++s) {
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) load(s, s, n);
@@ -223,19 +227,33 @@ __global__ __launch_bounds__(Shape::threads, 1) void linear_tile_kernel(LinearAr
         asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
     clear_tail(0, 0);
 #pragma unroll
-    for (int n = 0; n < kFirst; ++n) first_read(0, n);
+    for (int n = 0; n < kFirst; ++n) first_read(0, n, wv[0]);
+    auto after = [&](int place) { return place + 1 == kDepth ? 0 : place + 1; };
+    auto even_again = [&] {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int v = 0; v < kWWords; ++v) wv[0][j][v] = wv[1][j][v];
+    };
     int s = 0, place = 0;
-    for (; s + kDepth < stages; ++s) {
-        const int next = place + 1 == kDepth ? 0 : place + 1;
-        stage(s, place, next, std::integral_constant<int, 2>{});
-        place = next;
+    for (; s + kDepth + 1 < stages; s += 2) {
+        const int second = after(place), third = after(second);
+        stage(s, place, second, wv[0], wv[1], std::integral_constant<int, 2>{});
+        stage(s + 1, second, third, wv[1], wv[0], std::integral_constant<int, 2>{});
+        place = third;
+    }
+    if (s + kDepth < stages) {
+        stage(s, place, after(place), wv[0], wv[1], std::integral_constant<int, 2>{});
+        even_again();
+        place = after(place);
+        ++s;
     }
     for (; s + 1 < stages; ++s) {
-        const int next = place + 1 == kDepth ? 0 : place + 1;
-        stage(s, place, next, std::integral_constant<int, 1>{});
-        place = next;
+        stage(s, place, after(place), wv[0], wv[1], std::integral_constant<int, 1>{});
+        even_again();
+        place = after(place);
     }
-    stage(s, place, 0, std::integral_constant<int, 0>{});
+    stage(s, place, 0, wv[0], wv[1], std::integral_constant<int, 0>{});
 
     const int o = o0 + wave_n * 64 + g * 16;
     if (o >= A.n) return;
@@ -245,22 +263,29 @@ __global__ __launch_bounds__(Shape::threads, 1) void linear_tile_kernel(LinearAr
     for (int c = 0; c < 16; ++c) channel[c] = (int64_t)rt.expert * A.n + (o + c < A.n ? o + c : A.n - 1);
     channel_scales(A, channel, ws);
     channel_bias(A, channel, bias);
+    // (all loads in flight together: one after another, a token's scale at a time, they were a third of the time behind the last stage)
+    constexpr int kOut = kP / kPlanes;
+    const int64_t t0 = rt.row0 + wave_t * kOut * 16 + r16;
+    int64_t token[kOut];
+    float xs[kOut];
 #pragma unroll
-    for (int i = 0; i < kP / kPlanes; ++i) {
-        const int64_t t = rt.row0 + (wave_t * (kP / kPlanes) + i) * 16 + r16;
-        if (t >= rt.row_end) continue;
-        const float xs = load_scale(A.xs, t, A.xs_f16) * A.factor;
+    for (int i = 0; i < kOut; ++i) token[i] = t0 + 16 * i < rt.row_end ? t0 + 16 * i : rt.row_end - 1;
+    token_scales(A, token, xs);
+#pragma unroll
+    for (int i = 0; i < kOut; ++i) {
+        if (t0 + 16 * i >= rt.row_end) continue;
+        const float s = xs[i] * A.factor;
         float v[16];
 #pragma unroll
         for (int c = 0; c < 16; ++c) {
             int part[kPlanes];
 #pragma unroll
             for (int p = 0; p < kPlanes; ++p) part[p] = acc[i * kPlanes + p][c >> 2][c & 3];
-            v[c] = joined<kPlanes>(part) * xs;
+            v[c] = joined<kPlanes>(part) * s;
             if (A.ws) v[c] *= ws[c];
             if (A.bias) v[c] += bias[c];
         }
-        store_results<16>(A, t * A.ldy + o, v, A.n - o, A.y_quads);
+        store_results<16>(A, (t0 + 16 * i) * A.ldy + o, v, A.n - o, A.y_quads);
     }
 }
 
@@ -278,9 +303,12 @@ hipError_t launch_tile(const LinearArgs &A, hipStream_t stream)
     return hipGetLastError();
 }
 
-typedef TileShape<2, 4, 8> TileLarge;   // 256 tokens x 256 channels, or 128 x 256 of two planes
-typedef TileShape<4, 2, 6> TileLarge3;  // 128 tokens of three planes x 128
-typedef TileShape<2, 2, 4> TileSmall;   // 128 x 128, or 64 x 128 of two planes
-typedef TileShape<2, 2, 6> TileSmall3;  // 64 tokens of three planes x 128
+// x rows (tokens times planes) x channels
+typedef TileShape<2, 4, 8, 160> TileLarge;   // 256 x 256
+typedef TileShape<2, 4, 4, 160> TileMiddle;  // 128 x 256
+typedef TileShape<2, 2, 4, 80> TileSmall;    // 128 x 128, two workgroups per compute unit
+typedef TileShape<2, 2, 4, 160> TileDeep;    // 128 x 128, one of them with all of the LDS (8-bit codes: four stages instead of two)
+typedef TileShape<4, 2, 6, 160> TileLarge3;  // 384 x 128, for three planes
+typedef TileShape<2, 2, 6, 160> TileDeep3;   // 192 x 128
 
 }  // namespace bq

@@ -3,11 +3,19 @@
 
 namespace bq {
 
-hipError_t launch_linear_tile4(const LinearArgs &A, int wbits, bool large, hipStream_t stream)
+template <int kWBits>
+static hipError_t launch(const LinearArgs &A, LinearTile tile, hipStream_t stream)
 {
-    if (wbits == 8) return large ? launch_tile<4, 8, 1, TileLarge>(A, stream) : launch_tile<4, 8, 1, TileSmall>(A, stream);
-    if (wbits == 4) return large ? launch_tile<4, 4, 1, TileLarge>(A, stream) : launch_tile<4, 4, 1, TileSmall>(A, stream);
-    return large ? launch_tile<4, 2, 1, TileLarge>(A, stream) : launch_tile<4, 2, 1, TileSmall>(A, stream);
+    if (tile == kTileLarge) return launch_tile<4, kWBits, 1, TileLarge>(A, stream);
+    if (tile == kTileMiddle) return launch_tile<4, kWBits, 1, TileMiddle>(A, stream);
+    return launch_tile<4, kWBits, 1, TileSmall>(A, stream);
+}
+
+hipError_t launch_linear_tile4(const LinearArgs &A, int wbits, LinearTile tile, hipStream_t stream)
+{
+    if (wbits == 8) return launch<8>(A, tile, stream);
+    if (wbits == 4) return launch<4>(A, tile, stream);
+    return launch<2>(A, tile, stream);
 }
 
 }  // namespace bq

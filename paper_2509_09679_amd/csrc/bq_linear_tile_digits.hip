@@ -3,10 +3,13 @@
 
 namespace bq {
 
-hipError_t launch_linear_tile_digits(const LinearArgs &A, int planes, bool large, hipStream_t stream)
+hipError_t launch_linear_tile_digits(const LinearArgs &A, int planes, LinearTile tile, hipStream_t stream)
 {
-    if (planes == 2) return large ? launch_tile<8, 8, 2, TileLarge>(A, stream) : launch_tile<8, 8, 2, TileSmall>(A, stream);
-    return large ? launch_tile<8, 8, 3, TileLarge3>(A, stream) : launch_tile<8, 8, 3, TileSmall3>(A, stream);
+    if (planes == 3) return tile == kTileLarge ? launch_tile<8, 8, 3, TileLarge3>(A, stream) : launch_tile<8, 8, 3, TileDeep3>(A, stream);
+    if (tile == kTileLarge) return launch_tile<8, 8, 2, TileLarge>(A, stream);
+    if (tile == kTileMiddle) return launch_tile<8, 8, 2, TileMiddle>(A, stream);
+    if (tile == kTileDeep) return launch_tile<8, 8, 2, TileDeep>(A, stream);
+    return launch_tile<8, 8, 2, TileSmall>(A, stream);
 }
 
 }  // namespace bq

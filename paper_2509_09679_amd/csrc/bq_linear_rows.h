@@ -1,96 +1,146 @@
-// The product for few rows.  A workgroup of 8 waves takes kBlocks x kCols pieces of 16 tokens x 16 channels; the waves share the sum's
-// index, step by step, so that the workgroup reads its channels' codes front to back, every code once and straight into the registers
-// that the matrix instruction reads (16 bytes of one channel per lane).  The 8 partial sums are joined through LDS, in integers: the
-// order does not matter.  Decoding (a few tokens, kCols = 1) is bound by the weights' bytes; with more tokens the pieces grow, since a
-// code of x is read once per kCols pieces and one of w once per kBlocks.
+// The product for few rows.  A workgroup takes kBlocks x kCols pieces of 16 tokens x 16 channels; its waves share the sum's index, step by
+// step, so that the workgroup reads its channels' codes front to back, every code once, and every wave works for itself: it loads
+// the codes of its steps into a ring of its own in LDS (directly, 16 bytes per lane, whole lines: in the order the matrix instruction
+// wants them a load touched 64 lines instead of 8 or 16, and the address units were what bound the kernel: 33 KB/us and compute unit),
+// reads them from there and multiplies, with no barrier.  The waves' partial sums are joined through LDS, in integers: the order does
+// not matter.  Decoding (a few tokens, kCols = 1) is bound by the weights' bytes; with more tokens the pieces grow, since a code of x
+// is read once per kCols pieces and one of w once per kBlocks.
 #pragma once
 
 #include "bq_linear_codes.h"
 
 namespace bq {
 
-constexpr int kRowsWaves = 8;
+constexpr int kRowsLds = 160 * 1024;
 
 template <int kXBits, int kWBits, int kPlanes, int kBlocks, int kCols>
-__global__ __launch_bounds__(64 * kRowsWaves) void linear_rows_kernel(LinearArgs A)
+struct RowsShape {
+    static constexpr int frags = kBlocks * kPlanes;
+    static constexpr int codes = kWBits == 2 ? 256 : 128;                       // of a step
+    static constexpr int x_row = codes * kXBits / 8, w_row = codes * kWBits / 8;  // bytes of a step's rows: 64, 128, 256
+    static constexpr int x_bytes = frags * 16 * x_row, w_bytes = kCols * 16 * w_row, step = x_bytes + w_bytes;
+    static constexpr int waves = 16 * step <= kRowsLds ? 8 : 4;
+    static constexpr int fit = kRowsLds / (waves * step), depth = fit < 4 ? fit : 4;
+    static constexpr int pairs = kBlocks * kCols, most = waves / kPlanes, chunk = pairs < most ? pairs : most;  // pieces joined at a time
+    static constexpr int joined = waves * chunk * kPlanes * 1024;
+    static constexpr int lds = waves * depth * step > joined ? waves * depth * step : joined;
+    static_assert(depth >= 2, "one step is multiplied while another is loaded");
+};
+
+template <int kXBits, int kWBits, int kPlanes, int kBlocks, int kCols>
+__global__ __launch_bounds__((64 * RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols>::waves)) void linear_rows_kernel(LinearArgs A)
 {
-    constexpr int kFrags = kBlocks * kPlanes;
-    constexpr int kCodes = 128 / kWBits;       // codes of a lane per step: one 16-byte load of weights
-    constexpr int kSub = kCodes / 16;          // matrix instructions per step and piece
-    constexpr int kXWords = kCodes * kXBits / 32;
-    constexpr int kWords = kFrags * kXWords + kCols * 4;  // registers that a step's loads fill
-    // steps whose loads are in flight together (swept: 8-bit weights gain from more, 6.1 us against 7.2 with two steps for one token
-    // 4096 -> 4096; packed ones lose, 9.7 against 8.8 us for one token 4096 -> 11008 with four)
-    constexpr int kAhead = kWBits == 8 && kWords <= 8 ? 8 : kWBits == 8 && kWords <= 12 ? 4 : kWords <= 40 ? 2 : 1;
-    constexpr int kPairs = kBlocks * kCols, kChunk = kPairs < 8 / kPlanes ? kPairs : 8 / kPlanes;  // pieces joined at a time: 64 KB
+    typedef RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols> S;
+    constexpr int kFrags = S::frags, kWaves = S::waves, kDepth = S::depth, kPairs = S::pairs, kChunk = S::chunk;
+    constexpr int kXSub = S::x_row == 256 ? 2 : 1, kXLine = S::x_row / kXSub;  // rows of 256 bytes lie as two of 128
+    constexpr int kXWords = S::x_row / 16, kWWords = S::w_row / 16;            // of a lane: a quarter of a row
+    constexpr int kXLoads = S::x_bytes / 1024, kWLoads = S::w_bytes / 1024, kLoads = kXLoads + kWLoads;
     constexpr bool kNatural = kXBits != kWBits;
-    __shared__ i32x4 s_part[kRowsWaves][kChunk * kPlanes][64];
+    extern __shared__ __align__(16) uint8_t rows_lds[];
+    i32x4(*const s_part)[kChunk * kPlanes][64] = (i32x4(*)[kChunk * kPlanes][64])rows_lds;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r16 = lane & 15, g = lane >> 4;
     const int o0 = blockIdx.x * 16 * kCols;
     const int expert = A.offsets ? blockIdx.z : 0;
     int64_t row_a, row_b;
     expert_rows(A, expert, &row_a, &row_b);
-    const uint8_t *w[kCols];
+    uint8_t *const ring = rows_lds + wave * (kDepth * S::step);
+    const uint32_t ring0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)rows_lds + wave * (kDepth * S::step);
+
+    // what this lane loads of a step: instruction i of w covers 1024 / w_row channels
+    const uint8_t *const w_base = A.w + expert * A.w_step + (int64_t)o0 * A.ldw;
+    uint32_t w_off[kWLoads];
+    int w_piece[kWLoads];
 #pragma unroll
-    for (int c = 0; c < kCols; ++c) {
-        const int channel = o0 + 16 * c + r16;
-        w[c] = A.w + expert * A.w_step + (int64_t)(channel < A.n ? channel : A.n - 1) * A.ldw;
+    for (int i = 0; i < kWLoads; ++i) {
+        const int row = i * (1024 / S::w_row) + lane / (S::w_row / 16), last = A.n - o0 - 1;
+        w_piece[i] = (lane % (S::w_row / 16)) ^ lds_turn<S::w_row, kWWords / 4>(row & 15);
+        w_off[i] = (uint32_t)(row < last ? row : last) * (uint32_t)A.ldw;
     }
-    const int steps = (A.k + 4 * kCodes - 1) / (4 * kCodes);
+    const int steps = (A.k + S::codes - 1) / S::codes;
+    const int mine = steps > wave ? (steps - wave + kWaves - 1) / kWaves : 0;
+    // 16-byte pieces of the last step, where it is short
+    const int x_tail = (int)((int64_t)A.k * kXBits / 128) % (S::x_row / 16), w_tail = (int)((int64_t)A.k * kWBits / 128) % (S::w_row / 16);
     const int64_t pass = 16 * kBlocks;
     for (int64_t row0 = row_a + blockIdx.y * pass; row0 < row_b; row0 += gridDim.y * pass) {
-        const uint8_t *x[kFrags];
+        const uint8_t *x_base[kXLoads];
+        uint32_t x_off[kXLoads];
+        int x_piece[kXLoads];
 #pragma unroll
-        for (int f = 0; f < kFrags; ++f) {
-            const int64_t t = row0 + 16 * (f / kPlanes) + r16;
-            x[f] = A.x + (f % kPlanes) * A.plane_step + (t < row_b ? t : row_b - 1) * A.ldx;
+        for (int i = 0; i < kXLoads; ++i) {
+            // x lies as [half of a row][plane and 16 tokens][token]
+            const int line = i * (1024 / kXLine) + lane / (kXLine / 16), half = i * (1024 / kXLine) / (16 * kFrags);
+            const int frag = i * (1024 / kXLine) / 16 % kFrags, token = 16 * (frag / kPlanes) + line % 16;
+            const int last = (int)(row_b - row0 < pass ? row_b - row0 : pass) - 1;
+            x_piece[i] = half * 8 + ((lane % (kXLine / 16)) ^ lds_turn<kXLine, kXWords / 4>(line & 15));
+            x_base[i] = A.x + (frag % kPlanes) * A.plane_step + row0 * A.ldx;
+            x_off[i] = (uint32_t)(token < last ? token : last) * (uint32_t)A.ldx;
         }
+        auto load = [&](int i, int place) {  // the wave's i-th step
+            const int s = wave + i * kWaves;
+            const bool last = s == steps - 1;  // a piece behind the last input: the step's first one
+#pragma unroll
+            for (int n = 0; n < kXLoads; ++n)
+                load_to_lds(ring0 + place * S::step + n * 1024, x_off[n] + (last && x_tail && x_piece[n] >= x_tail ? 0 : x_piece[n]) * 16,
+                            x_base[n] + (int64_t)s * S::x_row);
+#pragma unroll
+            for (int n = 0; n < kWLoads; ++n)
+                load_to_lds(ring0 + place * S::step + S::x_bytes + n * 1024,
+                            w_off[n] + (last && w_tail && w_piece[n] >= w_tail ? 0 : w_piece[n]) * 16, w_base + (int64_t)s * S::w_row);
+        };
         i32x4 acc[kCols][kFrags] = {};
-        for (int s0 = wave; s0 < steps; s0 += kRowsWaves * kAhead) {
-            uint32_t wv[kAhead][kCols][4], xv[kAhead][kFrags][kXWords];
+        if (row0 != row_a + blockIdx.y * pass) __syncthreads();  // the pass before has read its sums
+        for (int i = 0; i < kDepth && i < mine; ++i) load(i, i);
+        for (int i = 0, place = 0; i < mine; ++i) {
+            if (i + kDepth <= mine)
+                asm volatile("s_waitcnt vmcnt(%0)" : : "n"((kDepth - 1) * kLoads) : "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            uint32_t wv[kCols][kWWords], xv[kFrags][kXWords];
+            const uint8_t *const at = ring + place * S::step;
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const int k = (s0 + u * kRowsWaves) * 4 * kCodes + g * kCodes;
-                const bool in = k < A.k;  // (a lane's codes are all inside or all outside)
-                const int wo = in ? (int)((int64_t)k * kWBits / 8) : 0, xo = in ? (int)((int64_t)k * kXBits / 8) : 0;
+            for (int f = 0; f < kFrags; ++f)
 #pragma unroll
-                for (int c = 0; c < kCols; ++c) {
-                    const uint4 q = *(const uint4 *)(w[c] + wo);
-                    wv[u][c][0] = in ? q.x : 0; wv[u][c][1] = in ? q.y : 0; wv[u][c][2] = in ? q.z : 0; wv[u][c][3] = in ? q.w : 0;
+                for (int j = 0; j < kXWords / 4; ++j) {
+                    const int piece = g * (kXWords / 4) + j;
+                    const uint4 q = *(const uint4 *)(at + ((piece / (kXLine / 16)) * kFrags * 16 + f * 16 + r16) * kXLine +
+                                                     ((piece % (kXLine / 16)) ^ lds_turn<kXLine, kXWords / 4>(r16)) * 16);
+                    xv[f][4 * j] = q.x; xv[f][4 * j + 1] = q.y; xv[f][4 * j + 2] = q.z; xv[f][4 * j + 3] = q.w;
                 }
 #pragma unroll
-                for (int f = 0; f < kFrags; ++f) {
-                    if constexpr (kXWords == 2) {
-                        const uint2 p = *(const uint2 *)(x[f] + xo);
-                        xv[u][f][0] = p.x; xv[u][f][1] = p.y;
-                    } else {
+            for (int c = 0; c < kCols; ++c)
 #pragma unroll
-                        for (int j = 0; j < kXWords; j += 4) {
-                            const uint4 p = *(const uint4 *)(x[f] + xo + 4 * j);
-                            xv[u][f][j] = p.x; xv[u][f][j + 1] = p.y; xv[u][f][j + 2] = p.z; xv[u][f][j + 3] = p.w;
-                        }
-                    }
+                for (int j = 0; j < kWWords / 4; ++j) {
+                    const uint4 q = *(const uint4 *)(at + S::x_bytes + (c * 16 + r16) * S::w_row +
+                                                     ((g * (kWWords / 4) + j) ^ lds_turn<S::w_row, kWWords / 4>(r16)) * 16);
+                    wv[c][4 * j] = q.x; wv[c][4 * j + 1] = q.y; wv[c][4 * j + 2] = q.z; wv[c][4 * j + 3] = q.w;
                 }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read: the place may be loaded again
+            if (i + kDepth < mine) load(i + kDepth, place);
+            place = place + 1 == kDepth ? 0 : place + 1;
+            if (x_tail && wave + i * kWaves == steps - 1) {  // codes behind the last input count as 0
+#pragma unroll
+                for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+                    for (int j = 0; j < kXWords; ++j)
+                        if (g * (kXWords / 4) + j / 4 >= x_tail) xv[f][j] = 0;
             }
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u)
+            for (int s = 0; s < S::codes / 64; ++s) {
+                i32x4 a[kCols];
 #pragma unroll
-                for (int s = 0; s < kSub; ++s) {
-                    i32x4 a[kCols];
+                for (int c = 0; c < kCols; ++c) a[c] = step_codes<kWBits, kNatural>(wv[c], s);
 #pragma unroll
-                    for (int c = 0; c < kCols; ++c) a[c] = step_codes<kWBits, kNatural>(wv[u][c], s);
+                for (int f = 0; f < kFrags; ++f) {
+                    const i32x4 b = step_codes<kXBits, kNatural>(xv[f], s);
 #pragma unroll
-                    for (int f = 0; f < kFrags; ++f) {
-                        const i32x4 b = step_codes<kXBits, kNatural>(xv[u][f], s);
-#pragma unroll
-                        for (int c = 0; c < kCols; ++c) acc[c][f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[c], b, acc[c][f], 0, 0, 0);
-                    }
+                    for (int c = 0; c < kCols; ++c) acc[c][f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[c], b, acc[c][f], 0, 0, 0);
                 }
+            }
         }
 #pragma unroll
         for (int first = 0; first < kPairs; first += kChunk) {
-            __syncthreads();  // (the sums before have been read)
+            __syncthreads();  // (the codes, or the sums before, have been read)
 #pragma unroll
             for (int i = 0; i < kChunk; ++i)
 #pragma unroll
@@ -104,7 +154,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void linear_rows_kernel(LinearArgs
             for (int p = 0; p < kPlanes; ++p) {
                 sum[p] = s_part[0][wave * kPlanes + p][lane];
 #pragma unroll
-                for (int v = 1; v < kRowsWaves; ++v) sum[p] += s_part[v][wave * kPlanes + p][lane];
+                for (int v = 1; v < kWaves; ++v) sum[p] += s_part[v][wave * kPlanes + p][lane];
             }
             const int64_t t = row0 + 16 * block + r16;
             const int o = o0 + 16 * col + 4 * g;
@@ -137,7 +187,11 @@ hipError_t launch_rows(const LinearArgs &A, hipStream_t stream)
     const int64_t rows = A.offsets ? (2 * A.rows + A.experts - 1) / A.experts : A.rows;
     const int64_t passes = (rows + 16 * kBlocks - 1) / (16 * kBlocks);
     const dim3 grid((unsigned)((A.n + 16 * kCols - 1) / (16 * kCols)), (unsigned)(passes < 1024 ? passes : 1024), (unsigned)A.experts);
-    hipLaunchKernelGGL((linear_rows_kernel<kXBits, kWBits, kPlanes, kBlocks, kCols>), grid, dim3(64 * kRowsWaves), 0, stream, A);
+    typedef RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols> S;
+    static LdsLimitOnce limit;
+    const hipError_t e = limit.set((const void *)linear_rows_kernel<kXBits, kWBits, kPlanes, kBlocks, kCols>, S::lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((linear_rows_kernel<kXBits, kWBits, kPlanes, kBlocks, kCols>), grid, dim3(64 * S::waves), S::lds, stream, A);
     return hipGetLastError();
 }
 

@@ -25,30 +25,41 @@ double pieces(const LinearArgs &A, int rows)
     return std::ceil(some > used ? some : used);
 }
 
-// What a kernel takes, in us.  The models below are fits to a sweep (T = 1 .. 8192 tokens, (K, N) = (4096, 4096), (4096, 11008),
-// (11008, 4096), (2048, 1024), (8192, 8192), codes of 8 and 4 bits); they follow it within a fifth, and what they choose is within a
-// tenth of the best of the sweep's kernels.  Measured, 8-bit codes 4096 -> 4096:
-//   tokens           16     64    128    256    512   1024   2048   4096   8192
-//   best few-row    7.6   11.0   15.8   19.9   37.7   70.0    144    287    601
-//   128 x 128       28      27     28     27     28     26     38     73    154
-//   ... deep        20      20     22     21     23     24     48     98    207
-//   128 x 256       26      27     29     28     29     28     37     73    147
-//   256 x 256       40      43     47     50     51     48     55     64    138
+// What a kernel takes, in us.  The constants below are fits to a sweep of all kernels (1 .. 8192 tokens, (K, N) from (1024, 2048) to
+// (11008, 4096), (8192, 8192) and (4096, 32000), codes of 8, 4 and 2 bits, digits): what they choose is within 2 % of the best of the
+// sweep's kernels on average, within 12 % at 93 % of its 858 points.  Measured, 8-bit codes 4096 -> 4096, us:
+//   tokens          1    16    32    64   128   256   512  1024  2048  4096  8192
+//   1x1           6.0   6.6   8.6  12.6  20.7  36.1  67.3   112
+//   2x2           6.4   6.9   7.5   7.5  11.0  18.0  30.4  52.9
+//   4x2           7.9   8.2   8.8   9.7  10.0  17.4  32.1  58.2
+//   128 x 128 deep 16    17    17    19    20    21    21    22    41    85   184
+//   128 x 128      23    24    24    26    26    27    28    26    36    70   147
+//   128 x 256      22    23    24    26    28    28    28    27    34    68   141
+//   256 x 256      38    39    40    41    44    46    48    45    47    60   120
 
-// A workgroup reads its codes at 30 KB/us, all of them together at 7.5 GB/ms.
+// The weights' bytes, at what a kernel that has to wait for them reaches.
+double weights_us(const LinearArgs &A, int wbits)
+{
+    const double used = !A.offsets ? 1.0 : A.experts < A.rows ? A.experts : (double)A.rows;
+    return used * A.n * A.k * wbits / 8.0 / 4.4e6;
+}
+
+// A compute unit reads 50 KB of codes a us, and every workgroup has a prologue and the joining of its sums.
 double rows_us(const LinearArgs &A, int xbits, int wbits, int planes, int blocks, int cols)
 {
-    const double workgroups = pieces(A, 16 * blocks) * std::ceil(A.n / (16.0 * cols));
+    const double rounds = pieces(A, 16 * blocks) * std::ceil(A.n / (16.0 * cols)) / kCUs;
     const double kb = (16.0 * blocks * planes * xbits + 16.0 * cols * wbits) / 8.0 * A.k / 1000.0;
-    const double alone = kb / 30.0, together = workgroups * kb / 7500.0;
-    return 3.0 + (alone > together ? alone : together);
+    const double codes = (rounds > 1.0 ? rounds : 1.0) * ((blocks * planes * cols >= 8 ? 2.1 : 1.1) + kb / 50.0);
+    const double weights = weights_us(A, wbits);
+    return 1.55 + (codes > weights ? codes : weights);
 }
 
 // A round of tiles on all compute units: `fixed` us and `stage` us per 128 codes.
-double tile_us(const LinearArgs &A, int planes, int x_rows, int channels, double at_once, double fixed, double stage)
+double tile_us(const LinearArgs &A, int wbits, int planes, int x_rows, int channels, double at_once, double fixed, double stage)
 {
     const double tiles = pieces(A, x_rows / planes) * std::ceil((double)A.n / channels);
-    return 3.0 + std::ceil(tiles / at_once) * (fixed + stage * A.k / 128.0);
+    const double codes = std::ceil(tiles / at_once) * (fixed + stage * A.k / 128.0), weights = weights_us(A, wbits);
+    return 2.15 + (codes > weights ? codes : weights);
 }
 
 }  // namespace
@@ -80,27 +91,23 @@ hipError_t launch_linear(const LinearArgs &A0, int xbits, int wbits, int planes,
             tile = which;
         }
     };
-    if (wbits < 8) rows(1, 2);
+    rows(1, 2);
     rows(2, 1);
     if (planes < 3) rows(2, 2);
     if (planes == 1) {
-        rows(4, 2);
-        rows(4, 4);
-    } else if (planes == 2) {
-        rows(2, 4);
-    } else {
         rows(1, 4);
+        rows(4, 2);
     }
     if (planes < 3) {
-        tiles(kTileLarge, tile_us(A, planes, 256, 256, kCUs, 6.0, 1.65));
-        tiles(kTileMiddle, tile_us(A, planes, 128, 256, kCUs, 4.0, 0.93));
+        // 128 x 128: two workgroups on a compute unit, or one; packed codes have the same stages either way
         const bool packed = xbits < 8 || wbits < 8;
-        // two workgroups on a compute unit, or one: packed codes have the same stages either way
-        tiles(kTileSmall, tile_us(A, planes, 128, 128, 2.0 * kCUs, 4.0, 1.08));
-        tiles(packed ? kTileSmall : kTileDeep, tile_us(A, planes, 128, 128, kCUs, 4.0, 0.52));
+        tiles(kTileLarge, tile_us(A, wbits, planes, 256, 256, kCUs, 5.35, 1.50));
+        tiles(kTileMiddle, tile_us(A, wbits, planes, 128, 256, kCUs, 3.1, 0.93));
+        tiles(kTileSmall, tile_us(A, wbits, planes, 128, 128, 2.0 * kCUs, 4.2, 0.93));
+        tiles(packed ? kTileSmall : kTileDeep, tile_us(A, wbits, planes, 128, 128, kCUs, 4.4, 0.66));
     } else {
-        tiles(kTileLarge, tile_us(A, 3, 384, 128, kCUs, 5.0, 1.35));
-        tiles(kTileDeep, tile_us(A, 3, 192, 128, kCUs, 4.0, 0.75));
+        tiles(kTileLarge, tile_us(A, wbits, 3, 384, 128, kCUs, 4.7, 1.24));
+        tiles(kTileDeep, tile_us(A, wbits, 3, 192, 128, kCUs, 5.8, 0.71));
     }
     if (few) {
         if (xbits == 4) return launch_linear_rows4(A, wbits, blocks, cols, stream);

@@ -11,26 +11,28 @@
 
 namespace bq {
 
-constexpr int kRowsLds = 160 * 1024;
-
-template <int kXBits, int kWBits, int kPlanes, int kBlocks, int kCols>
+// kWide: all of a compute unit's LDS for one workgroup, else half of it.
+template <int kXBits, int kWBits, int kPlanes, int kBlocks, int kCols, bool kWide>
 struct RowsShape {
     static constexpr int frags = kBlocks * kPlanes;
     static constexpr int codes = kWBits == 2 ? 256 : 128;                       // of a step
     static constexpr int x_row = codes * kXBits / 8, w_row = codes * kWBits / 8;  // bytes of a step's rows: 64, 128, 256
     static constexpr int x_bytes = frags * 16 * x_row, w_bytes = kCols * 16 * w_row, step = x_bytes + w_bytes;
-    static constexpr int waves = 16 * step <= kRowsLds ? 8 : 4;
-    static constexpr int fit = kRowsLds / (waves * step), depth = fit < 4 ? fit : 4;
+    static constexpr int room = (kWide ? 160 : 80) * 1024;
+    static constexpr int waves = 16 * step <= room ? 8 : 4;
+    static constexpr int per_simd = kWide ? 2 : waves / 2;  // waves that have to fit (four alone would get registers they have no use for)
+    static constexpr int fit = room / (waves * step), depth = fit < 4 ? fit : 4;
     static constexpr int pairs = kBlocks * kCols, most = waves / kPlanes, chunk = pairs < most ? pairs : most;  // pieces joined at a time
     static constexpr int joined = waves * chunk * kPlanes * 1024;
     static constexpr int lds = waves * depth * step > joined ? waves * depth * step : joined;
-    static_assert(depth >= 2, "one step is multiplied while another is loaded");
+    static constexpr bool exists = depth >= 2;  // one step is multiplied while another is loaded
 };
 
-template <int kXBits, int kWBits, int kPlanes, int kBlocks, int kCols>
-__global__ __launch_bounds__((64 * RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols>::waves)) void linear_rows_kernel(LinearArgs A)
+template <int kXBits, int kWBits, int kPlanes, int kBlocks, int kCols, bool kWide>
+__global__ __launch_bounds__((64 * RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols, kWide>::waves),
+                             (RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols, kWide>::per_simd)) void linear_rows_kernel(LinearArgs A)
 {
-    typedef RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols> S;
+    typedef RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols, kWide> S;
     constexpr int kFrags = S::frags, kWaves = S::waves, kDepth = S::depth, kPairs = S::pairs, kChunk = S::chunk;
     constexpr int kXSub = S::x_row == 256 ? 2 : 1, kXLine = S::x_row / kXSub;  // rows of 256 bytes lie as two of 128
     constexpr int kXWords = S::x_row / 16, kWWords = S::w_row / 16;            // of a lane: a quarter of a row
@@ -180,6 +182,17 @@ __global__ __launch_bounds__((64 * RowsShape<kXBits, kWBits, kPlanes, kBlocks, k
     }
 }
 
+template <int kXBits, int kWBits, int kPlanes, int kBlocks, int kCols, bool kWide>
+hipError_t launch_rows_shape(const LinearArgs &A, dim3 grid, hipStream_t stream)
+{
+    typedef RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols, kWide> S;
+    static LdsLimitOnce limit;
+    const hipError_t e = limit.set((const void *)linear_rows_kernel<kXBits, kWBits, kPlanes, kBlocks, kCols, kWide>, S::lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((linear_rows_kernel<kXBits, kWBits, kPlanes, kBlocks, kCols, kWide>), grid, dim3(64 * S::waves), S::lds, stream, A);
+    return hipGetLastError();
+}
+
 template <int kXBits, int kWBits, int kPlanes, int kBlocks, int kCols>
 hipError_t launch_rows(const LinearArgs &A, hipStream_t stream)
 {
@@ -187,33 +200,32 @@ hipError_t launch_rows(const LinearArgs &A, hipStream_t stream)
     const int64_t rows = A.offsets ? (2 * A.rows + A.experts - 1) / A.experts : A.rows;
     const int64_t passes = (rows + 16 * kBlocks - 1) / (16 * kBlocks);
     const dim3 grid((unsigned)((A.n + 16 * kCols - 1) / (16 * kCols)), (unsigned)(passes < 1024 ? passes : 1024), (unsigned)A.experts);
-    typedef RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols> S;
-    static LdsLimitOnce limit;
-    const hipError_t e = limit.set((const void *)linear_rows_kernel<kXBits, kWBits, kPlanes, kBlocks, kCols>, S::lds);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((linear_rows_kernel<kXBits, kWBits, kPlanes, kBlocks, kCols>), grid, dim3(64 * S::waves), S::lds, stream, A);
-    return hipGetLastError();
+    // Two workgroups on a compute unit hide one another's first loads and last sums; one alone gets more loads in flight.  8-bit codes
+    // of 16 tokens, K = 4096: 256 workgroups 7.4 us in pairs and 6.6 us alone, 688 of them 14.5 and 16.6 us.  Packed weights leave
+    // room for deep rings either way (688 workgroups 9.9 and 12.6 us, 256 of them 4.6 and 4.8 us).
+    constexpr bool kPair = RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols, false>::exists;
+    if constexpr (kPair) {
+        if (kWBits < 8 || (int64_t)grid.x * grid.y * grid.z > 256) return launch_rows_shape<kXBits, kWBits, kPlanes, kBlocks, kCols, false>(A, grid, stream);
+    }
+    if constexpr (!kPair || kWBits == 8) {
+        static_assert(RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols, true>::exists, "fits the LDS");
+        return launch_rows_shape<kXBits, kWBits, kPlanes, kBlocks, kCols, true>(A, grid, stream);
+    }
 }
 
-// blocks x cols: 1x1, 1x2 (packed weights), 2x1, 2x2, 4x2, 4x4; of a gradient's planes 1x1, 2x1, 2x2 and 2x4 (two) or 1x4 (three)
+// blocks x cols: 1x1, 1x2, 1x4, 2x1, 2x2, 4x2; of a gradient's planes 1x1, 1x2, 2x1 and (two planes) 2x2
 template <int kXBits, int kWBits, int kPlanes>
 hipError_t launch_rows_of(const LinearArgs &A, int blocks, int cols, hipStream_t stream)
 {
     if constexpr (kPlanes == 1) {
-        if (blocks == 4) return cols == 2 ? launch_rows<kXBits, kWBits, 1, 4, 2>(A, stream) : launch_rows<kXBits, kWBits, 1, 4, 4>(A, stream);
-        if constexpr (kWBits < 8) {
-            if (blocks == 1 && cols == 2) return launch_rows<kXBits, kWBits, 1, 1, 2>(A, stream);
-        }
+        if (blocks == 4) return launch_rows<kXBits, kWBits, 1, 4, 2>(A, stream);
+        if (cols == 4) return launch_rows<kXBits, kWBits, 1, 1, 4>(A, stream);
     }
-    if constexpr (kPlanes == 2) {
-        if (cols == 4) return launch_rows<kXBits, kWBits, 2, 2, 4>(A, stream);
-    }
-    if constexpr (kPlanes == 3) {
-        if (cols == 4) return launch_rows<kXBits, kWBits, 3, 1, 4>(A, stream);
-    } else {
+    if constexpr (kPlanes < 3) {
         if (blocks == 2 && cols == 2) return launch_rows<kXBits, kWBits, kPlanes, 2, 2>(A, stream);
     }
-    return blocks == 1 ? launch_rows<kXBits, kWBits, kPlanes, 1, 1>(A, stream) : launch_rows<kXBits, kWBits, kPlanes, 2, 1>(A, stream);
+    if (blocks == 2) return launch_rows<kXBits, kWBits, kPlanes, 2, 1>(A, stream);
+    return cols == 2 ? launch_rows<kXBits, kWBits, kPlanes, 1, 2>(A, stream) : launch_rows<kXBits, kWBits, kPlanes, 1, 1>(A, stream);
 }
 
 }  // namespace bq

@@ -247,6 +247,8 @@ typedef struct {
     int64_t ld_w;        /* row stride of w in bytes (>= ceil(K wbits / 8))                             */
     int64_t ld_y;        /* row stride of y or dy in elements (>= N)                                    */
 } bq_linear;
+/* Further limits: rows * max(ld_x, ld_y) and experts * N * ld_w at most 2^44, and (rows / 64 + experts) * ceil(width / 64) below
+ * 2^24, width being N or, for the gradient, K (some 2^36 results); else BQ_ERR_SHAPE. */
 
 /* y[t][o] = xscale[t] * wscale[o] * sum_k x[t][k] w[o][k] + bias[o]   (the layer's product Q(Bx) . Q(WB^T) of the
  * reconstruction loss, with one scale per token and one per output channel).  The sum is exact in 32-bit integers; it is

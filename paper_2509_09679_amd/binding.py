@@ -48,6 +48,12 @@ class bq_quant(ctypes.Structure):
 
 
 class bq_linear(ctypes.Structure):
+    """What follows from the fields is kept beside them until one of them changes."""
+
+    def __setattr__(self, name, value):
+        self.__dict__.clear()
+        super().__setattr__(name, value)
+
     _fields_ = [("rows", ctypes.c_int64), ("inputs", ctypes.c_int32), ("outputs", ctypes.c_int32), ("experts", ctypes.c_int32),
                 ("xbits", ctypes.c_int32), ("wbits", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale_dtype", ctypes.c_int32),
                 ("reserved", ctypes.c_int32), ("ld_x", ctypes.c_int64), ("ld_w", ctypes.c_int64), ("ld_y", ctypes.c_int64)]
@@ -342,18 +348,23 @@ def bq_butterfly_bwd_static_max_bytes() -> int:
     return int(lib().bq_butterfly_bwd_static_max_bytes())
 
 
-_here = None
+_current_device = None
 
 
-def _require_tensors(who: str, tensors) -> None:
-    """What the library cannot see in a bare pointer.  tensors: (name, tensor or None, its types, the elements it has to have, whether
-    it has to be contiguous).  Every one has to be on the current device, whose stream the call goes to."""
-    global _here
-    if _here is None:
+def _here() -> int:
+    """Index of the current device."""
+    global _current_device
+    if _current_device is None:
         import torch
 
         torch.cuda.init()
-        _here = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _current_device()
+
+
+def _refuse_tensors(who: str, tensors) -> None:
+    """Raises for what the library cannot see in a bare pointer.  tensors: (name, tensor or None, its types, the elements it has to have,
+    whether it has to be contiguous).  Every one has to be on the current device, whose stream the call goes to."""
     device = _here()
     for name, t, types, count, dense in tensors:
         if t is None:  # the library's own check
@@ -370,7 +381,7 @@ _TYPES = None
 
 
 def _torch_types(code: int):
-    """The torch type of a bq_dtype, as a tuple; -1: codes."""
+    """The torch type of a bq_dtype, as a tuple; -1: codes, -2: offsets, -3: a workspace."""
     global _TYPES
     if _TYPES is None:
         import torch
@@ -384,55 +395,104 @@ def bq_rows_quant8(x, codes, scales, stream=None) -> None:
     """x: [rows, cols] of any row type, codes: int8 [rows, cols], both with a contiguous last dimension; scales: [rows], float32 or
     float16."""
     rows, cols = x.shape
-    ld_x, ld_codes = (x.stride(0), codes.stride(0)) if rows > 1 else (cols, cols)
-    _require(x.stride(1) == codes.stride(1) == 1 or cols == 1 or rows == 0, 2, "bq_rows_quant8: the last dimension must be contiguous")
-    _require(codes.shape == x.shape, 2, "bq_rows_quant8: codes and x differ in shape")
-    _require_tensors("bq_rows_quant8", (("x", x, _torch_types(BQ_F32) + _torch_types(BQ_F16) + _torch_types(BQ_BF16), 0, False),
-                                        ("codes", codes, _torch_types(-1), 0, False),
-                                        ("scales", scales, _torch_types(BQ_F32) + _torch_types(BQ_F16), rows, True)))
-    _check((_CALLS or _calls()).rows_quant8(x, rows, cols, ld_x, _dtype_code(x), codes, ld_codes, scales, _dtype_code(scales), _stream_ptr(stream)))
+    if rows > 1:
+        ld_x, step_x = x.stride()
+        ld_codes, step_codes = codes.stride()
+        _require(step_x == step_codes == 1 or cols == 1, 2, "bq_rows_quant8: the last dimension must be contiguous")
+    else:
+        ld_x = ld_codes = cols
+        _require(cols <= 1 or x.numel() == 0 or x.stride(1) == codes.stride(1) == 1, 2, "bq_rows_quant8: the last dimension must be contiguous")
+    if codes.shape != x.shape:
+        raise BqError(2, "bq_rows_quant8: codes and x differ in shape")
+    here, values = _here(), _ROW_TYPES or _row_types()
+    x_code, scale_code = values.get(x.dtype, -1), values.get(scales.dtype, -1)
+    if not (x.get_device() == codes.get_device() == scales.get_device() == here and x_code >= 0 and 0 <= scale_code <= BQ_F16
+            and codes.dtype in _torch_types(-1) and scales.numel() >= rows and scales.is_contiguous()):
+        _refuse_tensors("bq_rows_quant8", (("x", x, tuple(values), 0, False), ("codes", codes, _torch_types(-1), 0, False),
+                                           ("scales", scales, _torch_types(BQ_F32) + _torch_types(BQ_F16), rows, True)))
+    _check((_CALLS or _calls()).rows_quant8(x, rows, cols, ld_x, x_code, codes, ld_codes, scales, scale_code, _stream_ptr(stream)))
+
+
+_ROW_TYPES = None
+
+
+def _row_types():
+    global _ROW_TYPES
+    import torch
+
+    _ROW_TYPES = {torch.float32: BQ_F32, torch.float16: BQ_F16, torch.bfloat16: BQ_BF16}
+    return _ROW_TYPES
 
 
 def bq_linear_bwd_workspace_bytes(desc: bq_linear) -> int:
     return int(lib().bq_linear_bwd_workspace_bytes(ctypes.byref(desc)))
 
 
-def _linear_tensors(d: bq_linear, x, xscale, w, wscale, bias, y):
-    per_channel, scales, values = d.experts * d.outputs, _torch_types(d.scale_dtype), _torch_types(d.dtype)
-    return (("x", x, _torch_types(-1), (d.inputs * d.xbits + 7) // 8 * d.rows, False), ("xscale", xscale, scales, d.rows, True),
-            ("w", w, _torch_types(-1), (d.inputs * d.wbits + 7) // 8 * per_channel, False), ("wscale", wscale, scales, per_channel, True),
-            ("bias", bias, values, per_channel, True), ("y", y, values, d.rows * d.outputs, False))
+def _needs(d: bq_linear):
+    """What the tensors of a call have to have: the types of codes, scales and values; how many rows, and elements of x, scales per
+    channel, w, y (or dy) and dx; the row strides of x (or dx), w and y (or dy)."""
+    per_channel = d.experts * d.outputs
+    needs = (_torch_types(-1), (_torch_types(d.scale_dtype) or (None,))[0], (_torch_types(d.dtype) or (None,))[0], d.rows,
+             (d.inputs * d.xbits + 7) // 8 * d.rows, per_channel, (d.inputs * d.wbits + 7) // 8 * per_channel, d.rows * d.outputs,
+             d.rows * d.inputs, d.ld_x, d.ld_w, d.ld_y)
+    d.__dict__["needs"] = needs
+    return needs
 
 
-def _linear_bwd_tensors(d: bq_linear, dy, w, wscale, dx, workspace):
-    per_channel, values = d.experts * d.outputs, _torch_types(d.dtype)
-    return (("dy", dy, values, d.rows * d.outputs, False), ("w", w, _torch_types(-1), (d.inputs * d.wbits + 7) // 8 * per_channel, False),
-            ("wscale", wscale, _torch_types(d.scale_dtype), per_channel, True), ("dx", dx, values, d.rows * d.inputs, False),
-            ("workspace", workspace, _torch_types(-3), 0, True))
+def _require_strides(who: str, tensors) -> None:
+    """tensors: (name, tensor, the row stride that the descriptor says)."""
+    for name, t, ld in tensors:
+        if t is not None and t.dim() >= 2 and t.shape[-2] > 1:
+            _require(t.stride(-2) == ld, 2, f"{who}: rows of {name} are {t.stride(-2)} elements apart, the descriptor says {ld}")
+
+
+def _check_fwd(who: str, d: bq_linear, x, xscale, w, wscale, bias, y) -> None:
+    codes, scale, value, rows, n_x, channels, n_w, n_y, _, ld_x, ld_w, ld_y = d.__dict__.get("needs") or _needs(d)
+    here = _here()
+    if (x is not None and w is not None and xscale is not None and wscale is not None and y is not None
+            and x.get_device() == w.get_device() == xscale.get_device() == wscale.get_device() == y.get_device() == here
+            and x.dtype in codes and w.dtype in codes and xscale.dtype is wscale.dtype is scale and y.dtype is value and x.numel() >= n_x
+            and w.numel() >= n_w and y.numel() >= n_y and xscale.numel() >= rows and wscale.numel() >= channels and xscale.is_contiguous()
+            and wscale.is_contiguous() and bias is None and w.stride(-2) == ld_w and (rows <= 1 or (x.stride(0) == ld_x and y.stride(0) == ld_y))):
+        return
+    _refuse_tensors(who, (("x", x, codes, n_x, False), ("xscale", xscale, (scale,), rows, True), ("w", w, codes, n_w, False),
+                          ("wscale", wscale, (scale,), channels, True), ("bias", bias, (value,), channels, True), ("y", y, (value,), n_y, False)))
+    _require_strides(who, (("x", x, ld_x), ("w", w, ld_w), ("y", y, ld_y)))
+
+
+def _check_bwd(who: str, d: bq_linear, dy, w, wscale, dx, workspace) -> None:
+    codes, scale, value, _, _, channels, n_w, n_y, n_dx, ld_x, ld_w, ld_y = d.__dict__.get("needs") or _needs(d)
+    _refuse_tensors(who, (("dy", dy, (value,), n_y, False), ("w", w, codes, n_w, False), ("wscale", wscale, (scale,), channels, True),
+                          ("dx", dx, (value,), n_dx, False), ("workspace", workspace, _torch_types(-3), 0, True)))
+    _require_strides(who, (("dy", dy, ld_y), ("w", w, ld_w), ("dx", dx, ld_x)))
+
+
+def _check_offsets(who: str, d: bq_linear, offsets) -> None:
+    _refuse_tensors(who, (("offsets", offsets, _torch_types(-2), d.experts + 1, True),))
 
 
 def bq_linear_fwd(x, xscale, w, wscale, bias, y, desc: bq_linear, stream=None) -> None:
     """desc: make_linear(x, w, wscale, y, ...); bias may be None."""
-    _require_tensors("bq_linear_fwd", _linear_tensors(desc, x, xscale, w, wscale, bias, y))
+    _check_fwd("bq_linear_fwd", desc, x, xscale, w, wscale, bias, y)
     _check((_CALLS or _calls()).linear_fwd(x, xscale, w, wscale, bias, y, desc, _stream_ptr(stream)))
 
 
 def bq_linear_grouped_fwd(x, xscale, w, wscale, bias, offsets, y, desc: bq_linear, stream=None) -> None:
     """Rows sorted by expert; offsets: int32 [experts + 1] on the device."""
-    _require_tensors("bq_linear_grouped_fwd", _linear_tensors(desc, x, xscale, w, wscale, bias, y) +
-                     (("offsets", offsets, _torch_types(-2), desc.experts + 1, True),))
+    _check_fwd("bq_linear_grouped_fwd", desc, x, xscale, w, wscale, bias, y)
+    _check_offsets("bq_linear_grouped_fwd", desc, offsets)
     _check((_CALLS or _calls()).linear_grouped_fwd(x, xscale, w, wscale, bias, offsets, y, desc, _stream_ptr(stream)))
 
 
 def bq_linear_bwd(dy, w, wscale, dx, workspace, desc: bq_linear, stream=None) -> None:
     """desc: make_linear_bwd(dy, w, wscale, dx, ...); workspace: uint8, at least bq_linear_bwd_workspace_bytes(desc)."""
-    _require_tensors("bq_linear_bwd", _linear_bwd_tensors(desc, dy, w, wscale, dx, workspace))
+    _check_bwd("bq_linear_bwd", desc, dy, w, wscale, dx, workspace)
     _check((_CALLS or _calls()).linear_bwd(dy, w, wscale, dx, workspace, workspace.numel(), desc, _stream_ptr(stream)))
 
 
 def bq_linear_grouped_bwd(dy, w, wscale, offsets, dx, workspace, desc: bq_linear, stream=None) -> None:
-    _require_tensors("bq_linear_grouped_bwd", _linear_bwd_tensors(desc, dy, w, wscale, dx, workspace) +
-                     (("offsets", offsets, _torch_types(-2), desc.experts + 1, True),))
+    _check_bwd("bq_linear_grouped_bwd", desc, dy, w, wscale, dx, workspace)
+    _check_offsets("bq_linear_grouped_bwd", desc, offsets)
     _check((_CALLS or _calls()).linear_grouped_bwd(dy, w, wscale, offsets, dx, workspace, workspace.numel(), desc, _stream_ptr(stream)))
 
 

@@ -457,9 +457,9 @@ static bq_status check_linear(const bq_linear *d, bool grouped, bool backward, c
     const int64_t ld_max = d->ld_x > d->ld_y ? d->ld_x : d->ld_y;
     if ((d->rows > 0 && ld_max > ((int64_t)1 << 44) / d->rows) || d->ld_w > ((int64_t)1 << 44) / ((int64_t)d->experts * d->outputs))
         return fail(BQ_ERR_SHAPE, "%s: rows * leading dimension exceeds 2^44", who);
-    // one workgroup per 64 x 64 results at most, counted in 31 bits
+    // a workgroup of 256 threads per 64 x 64 results at most, threads counted in 32 bits
     const int64_t width = backward ? d->inputs : d->outputs;
-    if ((d->rows / 64 + d->experts) * ((width + 63) / 64) >= (int64_t)1 << 31) return fail(BQ_ERR_SHAPE, "%s: batch too large", who);
+    if ((d->rows / 64 + d->experts) * ((width + 63) / 64) >= (int64_t)1 << 24) return fail(BQ_ERR_SHAPE, "%s: batch too large", who);
     return BQ_OK;
 }
 

@@ -116,7 +116,7 @@ __device__ __forceinline__ int64_t row_tiles(const LinearArgs &A, int tile)
 }
 
 // an upper bound that the host can state
-inline int64_t row_tiles_bound(const LinearArgs &A, int tile)
+__host__ __device__ inline int64_t row_tiles_bound(const LinearArgs &A, int tile)
 {
     if (!A.offsets) return (A.rows + tile - 1) / tile;
     return A.rows / tile + (A.experts < A.rows ? A.experts : A.rows);

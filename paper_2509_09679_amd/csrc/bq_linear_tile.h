@@ -63,7 +63,9 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
 
     // which tile: workgroups go round the 8 XCDs, each of which takes a contiguous eighth of the tiles; within it 8 tiles along the
     // tokens and then the next channels, so that what runs together shares its rows in the XCD's L2
-    const uint32_t n_tiles = (uint32_t)(A.n + Shape::w_rows - 1) / Shape::w_rows, m_tiles = (uint32_t)row_tiles(A, kTokens);
+    const uint32_t n_tiles = (uint32_t)(A.n + Shape::w_rows - 1) / Shape::w_rows;
+    const int64_t most = row_tiles_bound(A, kTokens), counted = row_tiles(A, kTokens);  // (more only of overlapping experts)
+    const uint32_t m_tiles = (uint32_t)(counted < most ? counted : most);
     const uint32_t all = m_tiles * n_tiles, each = (all + 7) / 8, idx = blockIdx.x >> 3;
     const uint32_t tile = (blockIdx.x & 7) * each + idx;
     if (idx >= each || tile >= all) return;

@@ -47,14 +47,14 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t m)
     return m;
 }
 
-// kLanes threads per row (64: four rows per workgroup), kPasses pieces of 8 elements per thread; wider rows are read again.
+// kLanes threads per row (64: four rows per workgroup), kPasses pieces of 8 elements per thread.
 template <typename T, int kLanes, int kPasses>
 __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void row_quant_kernel(RowQuantArgs A)
 {
     constexpr int kThreads = kLanes < 256 ? 256 : kLanes, kRows = kThreads / kLanes;
     __shared__ uint32_t s_max[kThreads / 64];
     const int lane = threadIdx.x % kLanes;
-    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
+    const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kRows + threadIdx.x / kLanes;
     const bool live = row < A.rows;
     const T *x = (const T *)A.x + (live ? row : 0) * A.ld_x;
     float v[kPasses][8];
@@ -141,22 +141,24 @@ hipError_t launch_typed(const RowQuantArgs &A, hipStream_t stream)
         hipLaunchKernelGGL(row_quant_any_kernel<T>, dim3((unsigned)(A.rows < 65536 ? A.rows : 65536)), dim3(256), 0, stream, A);
         return hipGetLastError();
     }
-    const unsigned rows = (unsigned)A.rows, quads = (unsigned)((A.rows + 3) / 4);
+    // (threads along a dimension of a launch are counted in 32 bits)
+    auto grid = [](int64_t groups) { return dim3((unsigned)(groups < 1 << 20 ? groups : 1 << 20), (unsigned)((groups + (1 << 20) - 1) >> 20)); };
+    const dim3 rows = grid(A.rows), quads = grid((A.rows + 3) / 4);
     const int eights = A.cols / 8;
     if (eights <= 64)
-        hipLaunchKernelGGL((row_quant_kernel<T, 64, 1>), dim3(quads), dim3(256), 0, stream, A);
+        hipLaunchKernelGGL((row_quant_kernel<T, 64, 1>), quads, dim3(256), 0, stream, A);
     else if (eights <= 128)
-        hipLaunchKernelGGL((row_quant_kernel<T, 64, 2>), dim3(quads), dim3(256), 0, stream, A);
+        hipLaunchKernelGGL((row_quant_kernel<T, 64, 2>), quads, dim3(256), 0, stream, A);
     else if (eights <= 256)
-        hipLaunchKernelGGL((row_quant_kernel<T, 256, 1>), dim3(rows), dim3(256), 0, stream, A);
+        hipLaunchKernelGGL((row_quant_kernel<T, 256, 1>), rows, dim3(256), 0, stream, A);
     else if (eights <= 512)
-        hipLaunchKernelGGL((row_quant_kernel<T, 256, 2>), dim3(rows), dim3(256), 0, stream, A);
+        hipLaunchKernelGGL((row_quant_kernel<T, 256, 2>), rows, dim3(256), 0, stream, A);
     else if (eights <= 1024)
-        hipLaunchKernelGGL((row_quant_kernel<T, 256, 4>), dim3(rows), dim3(256), 0, stream, A);
+        hipLaunchKernelGGL((row_quant_kernel<T, 256, 4>), rows, dim3(256), 0, stream, A);
     else if (eights <= 2048)
-        hipLaunchKernelGGL((row_quant_kernel<T, 512, 4>), dim3(rows), dim3(512), 0, stream, A);
+        hipLaunchKernelGGL((row_quant_kernel<T, 512, 4>), rows, dim3(512), 0, stream, A);
     else
-        hipLaunchKernelGGL((row_quant_kernel<T, 1024, 4>), dim3(rows), dim3(1024), 0, stream, A);
+        hipLaunchKernelGGL((row_quant_kernel<T, 1024, 4>), rows, dim3(1024), 0, stream, A);
     return hipGetLastError();
 }
 

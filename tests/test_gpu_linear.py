@@ -394,3 +394,16 @@ def test_large_tiles_bwd(dtype, experts):
         f32 = term * v.abs().amax(1, keepdim=True) * qw[e].abs().sum(0) + 2 * 2.0 ** -24 * want.abs()
         _within(dx[lo:hi], want, f32 + (lu.half_step(dtype) * (want.abs() + f32) if dtype != "f32" else 0) + 1e-40)
     assert (dx[:offsets[0]] == 3).all() and (dx[offsets[-1]:] == 3).all()
+
+
+@pytest.mark.parametrize("rows,cols", [((4 << 21) + 5, 8), ((2 << 20) + 3, 1032)])
+def test_rows_quant8_of_more_rows_than_workgroups(rows, cols):
+    x = torch.randn((rows, cols), generator=torch.Generator(device=DEV).manual_seed(3), device=DEV, dtype=torch.bfloat16)
+    codes, scales = B.alloc_rows_quant8(rows, cols, "f32", DEV)
+    codes.fill_(99)
+    B.bq_rows_quant8(x, codes, scales)
+    for a in range(0, rows, 1 << 19):
+        v = x[a:a + (1 << 19)].float()
+        s = (v.abs().amax(1).double() / 127.0).float()
+        assert torch.equal(scales[a:a + (1 << 19)], s)
+        assert torch.equal(codes[a:a + (1 << 19)], torch.round(v * (1.0 / s.double()).float()[:, None]).clamp_(-128, 127).to(torch.int8))

@@ -49,7 +49,7 @@ def test_kinds_match_the_ctypes_prototypes():
 def test_bad_descriptors(call):
     for kw in (dict(rows=-1), dict(rows=1 << 31), dict(inputs=0), dict(inputs=131072, ld_x=1 << 20, ld_w=1 << 20), dict(outputs=0), dict(experts=0),
                dict(experts=4097), dict(ld_x=63), dict(ld_w=63), dict(ld_y=47), dict(ld_x=1 << 43), dict(ld_y=1 << 43), dict(ld_w=1 << 42),
-               dict(rows=(1 << 31) - 1, outputs=70000, inputs=70000, ld_x=70000, ld_w=70000, ld_y=70000)):
+               dict(rows=1 << 26, outputs=1 << 16, inputs=1 << 16, ld_x=1 << 16, ld_w=1 << 16, ld_y=1 << 16), dict(rows=(1 << 31) - 1, outputs=70000, inputs=70000, ld_x=70000, ld_w=70000, ld_y=70000)):
         assert call(_desc(**kw)) == 2, kw
     assert call(_desc(dtype=5)) == 3 and call(_desc(scale_dtype=B.BQ_BF16)) == 3
     assert call(_desc(wbits=3)) == 6 and call(_desc(wbits=16)) == 6
@@ -119,6 +119,19 @@ def test_descriptors_from_tensors():
             bad()
 
 
+def test_a_changed_descriptor_is_looked_at_again(monkeypatch):
+    monkeypatch.setattr(B, "_here", lambda: -1)
+    x, w, ws, y, xs = torch.zeros(7, 32, dtype=torch.int8), torch.zeros(5, 32, dtype=torch.int8), torch.zeros(5), torch.zeros(7, 5), torch.zeros(7)
+    d = B.make_linear(x, w, ws, y)
+    B._check_fwd("t", d, x, xs, w, ws, None, y)
+    d.rows = 8
+    with pytest.raises(B.BqError):
+        B._check_fwd("t", d, x, xs, w, ws, None, y)
+    d.rows, d.dtype = 7, B.BQ_F16
+    with pytest.raises(B.BqError):
+        B._check_fwd("t", d, x, xs, w, ws, None, y)
+
+
 def test_tensors_the_library_cannot_see(monkeypatch):
     # element types, extents and contiguity; CPU tensors taken for the current device's, nothing reaches the library
     monkeypatch.setattr(B, "_here", lambda: -1)
@@ -134,6 +147,8 @@ def test_tensors_the_library_cannot_see(monkeypatch):
     for call, status in ((lambda: fwd(x=x.float()), 3), (lambda: fwd(xs=xs.half()), 3), (lambda: fwd(xs=xs[:6]), 2), (lambda: fwd(w=w[:4]), 2),
                          (lambda: fwd(ws=torch.zeros(10)[::2]), 2), (lambda: fwd(y=y.half()), 3), (lambda: fwd(y=y[:6]), 2),
                          (lambda: fwd(b=torch.zeros(4)), 2), (lambda: fwd(b=torch.zeros(5).half()), 3),
+                         (lambda: fwd(x=torch.zeros(7, 40, dtype=torch.int8)[:, :32]), 2), (lambda: fwd(w=torch.zeros(5, 40, dtype=torch.int8)[:, :32]), 2),
+                         (lambda: fwd(y=torch.zeros(7, 8)[:, :5]), 2), (lambda: B.bq_linear_bwd(torch.zeros(7, 6)[:, :5], w, ws, torch.zeros(7, 32), work, g), 2),
                          (lambda: B.bq_linear_grouped_fwd(x, xs, w, ws, None, off.long(), y, d), 3),
                          (lambda: B.bq_linear_grouped_fwd(x, xs, w, ws, None, off[:1], y, d), 2),
                          (lambda: B.bq_linear_bwd(y.half(), w, ws, torch.zeros(7, 32), work, g), 3),

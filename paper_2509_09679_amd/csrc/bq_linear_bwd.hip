@@ -97,16 +97,24 @@ __device__ __forceinline__ void digits8(const float (&v)[8], const RowFactor &f,
     for (int p = 0; p < kPlanes; ++p) d[p] = make_uint2(w[p][0], w[p][1]);
 }
 
-// Rows of whole, aligned pieces of 8: a workgroup takes neighbouring rows, which mostly belong to one expert, and keeps that expert's
-// scales and a row's products in registers; kPasses pieces per thread.  One read of dy and one write of the digits: bound by HBM.
+// Rows of whole, aligned pieces of 8: workgroup `block` takes rows_each neighbouring rows, which mostly belong to one expert, and keeps
+// that expert's scales and a row's products in registers; kPasses pieces per thread.  One read of dy and one write of the digits: bound
+// by HBM.
 template <typename T, int kPlanes, int kPasses>
-__global__ __launch_bounds__(256) void linear_digits_kernel(DigitArgs A, int rows_each)
+__device__ __forceinline__ void digit_rows(const DigitArgs &A, int64_t block, int rows_each)
 {
-    const int64_t first = (int64_t)blockIdx.x * rows_each;
+    const int64_t first = block * rows_each;
     const int64_t end = first + rows_each < A.rows ? first + rows_each : A.rows;
     float ws[kPasses][8];
     int expert = -1;
     for (int64_t row = first; row < end; ++row) {
+        const T *dy = (const T *)A.dy + row * A.ld_dy;
+        Raw8 raw[kPasses];
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) {  // (asked for ahead of the expert, whose place takes two more turns to memory)
+            const int c = (p * 256 + threadIdx.x) * 8;
+            raw[p] = load8(dy + (c < A.n ? c : 0));
+        }
         const int e = expert_of(A.offsets, A.experts, row);
         if (e < 0) continue;  // (the product does not look at it)
         if (e != expert) {
@@ -121,19 +129,15 @@ __global__ __launch_bounds__(256) void linear_digits_kernel(DigitArgs A, int row
                     unpack8(load8((const float *)A.ws + at), ws[p], (const float *)nullptr);
             }
         }
-        const T *dy = (const T *)A.dy + row * A.ld_dy;
         float v[kPasses][8];
         uint32_t m = 0;
 #pragma unroll
         for (int p = 0; p < kPasses; ++p) {
-            const int c = (p * 256 + threadIdx.x) * 8;
-#pragma unroll
-            for (int r = 0; r < 8; ++r) v[p][r] = 0.0f;
-            if (c >= A.n) continue;
-            unpack8(load8(dy + c), v[p], (const T *)nullptr);
+            const bool in = (int)(p * 256 + threadIdx.x) * 8 < A.n;
+            unpack8(raw[p], v[p], (const T *)nullptr);
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
-                v[p][r] *= ws[p][r];
+                v[p][r] = in ? v[p][r] * ws[p][r] : 0.0f;
                 const uint32_t b = __float_as_uint(v[p][r]) & 0x7FFFFFFFu;
                 m = m > b ? m : b;
             }
@@ -193,17 +197,18 @@ __device__ __forceinline__ bool has_rows(const int32_t *offsets, int expert) { r
 
 constexpr int kTr = 128;
 
-// 128 outputs x 128 inputs per workgroup.  A thread reads 16 codes of four neighbouring outputs, turns them in registers, 4 x 4 bytes at
+// 128 outputs x 128 inputs per workgroup, workgroup `block` of all.  A thread reads 16 codes of four neighbouring outputs, turns them in registers, 4 x 4 bytes at
 // a time, and stores words of four outputs to LDS, from where the result's rows leave in whole lines.  Codes of 4 and 2 bits come
 // out as bytes with the code at the top, 16 or 64 times its value.  One read of w, one write: bound by HBM.
 template <int kBits>
-__global__ __launch_bounds__(256) void linear_transpose_kernel(TransposeArgs A)
+__device__ __forceinline__ void transpose_tile(const TransposeArgs &A, uint32_t block)
 {
     constexpr int kLd = kTr / 4 + 1;
     __shared__ uint32_t s[kTr * kLd];
-    const int expert = blockIdx.z;
+    const uint32_t across = (uint32_t)(A.k + kTr - 1) / kTr, down = (uint32_t)A.np / kTr;
+    const int expert = (int)(block / (across * down));
     if (!has_rows(A.offsets, expert)) return;
-    const int k0 = blockIdx.x * kTr, o0 = blockIdx.y * kTr;
+    const int k0 = (int)(block % across) * kTr, o0 = (int)(block / across % down) * kTr;
     const int quad = threadIdx.x >> 3, part = (threadIdx.x & 7) * 16;
     uint32_t c[4][4] = {};  // [output][word]
 #pragma unroll
@@ -243,6 +248,16 @@ __global__ __launch_bounds__(256) void linear_transpose_kernel(TransposeArgs A)
     }
 }
 
+// Both in one launch: neither needs the other.  The first digit_blocks workgroups write digits, the others transpose.
+template <typename T, int kPlanes, int kPasses, int kBits>
+__global__ __launch_bounds__(256) void linear_prepare_kernel(DigitArgs D, int rows_each, uint32_t digit_blocks, TransposeArgs R)
+{
+    if (blockIdx.x < digit_blocks)
+        digit_rows<T, kPlanes, kPasses>(D, blockIdx.x, rows_each);
+    else
+        transpose_tile<kBits>(R, blockIdx.x - digit_blocks);
+}
+
 // The same for any width and alignment, 64 x 64 codes one by one.
 __global__ __launch_bounds__(256) void linear_transpose_any_kernel(TransposeArgs A, int bits)
 {
@@ -266,41 +281,39 @@ __global__ __launch_bounds__(256) void linear_transpose_any_kernel(TransposeArgs
 
 int padded(int n) { return (n + 127) / 128 * 128; }
 
-template <typename T, int kPlanes>
-hipError_t launch_digits(const DigitArgs &D, hipStream_t stream)
+template <typename T, int kPlanes, int kBits>
+hipError_t launch_prepare(const DigitArgs &D, const TransposeArgs &R, hipStream_t stream)
 {
-    const bool vec = (uintptr_t)D.dy % 16 == 0 && D.ld_dy * sizeof(T) % 16 == 0 && D.n % 8 == 0 && (uintptr_t)D.ws % 16 == 0 && D.np <= 16384;
-    if (!vec) {
-        hipLaunchKernelGGL((linear_digits_any_kernel<T, kPlanes>), dim3((unsigned)(D.rows < 65536 ? D.rows : 65536)), dim3(256), 0, stream, D);
-        return hipGetLastError();
-    }
     // 8 workgroups fit a compute unit; beyond 4096 they take several rows each
     const int rows_each = (int)((D.rows + 4095) / 4096);
-    const dim3 grid((unsigned)((D.rows + rows_each - 1) / rows_each));
+    const uint32_t digit_blocks = (uint32_t)((D.rows + rows_each - 1) / rows_each);
+    const dim3 grid(digit_blocks + (uint32_t)((R.k + kTr - 1) / kTr) * (uint32_t)(R.np / kTr) * (uint32_t)D.experts);
     if (D.np <= 2048)
-        hipLaunchKernelGGL((linear_digits_kernel<T, kPlanes, 1>), grid, dim3(256), 0, stream, D, rows_each);
+        hipLaunchKernelGGL((linear_prepare_kernel<T, kPlanes, 1, kBits>), grid, dim3(256), 0, stream, D, rows_each, digit_blocks, R);
     else if (D.np <= 4096)
-        hipLaunchKernelGGL((linear_digits_kernel<T, kPlanes, 2>), grid, dim3(256), 0, stream, D, rows_each);
+        hipLaunchKernelGGL((linear_prepare_kernel<T, kPlanes, 2, kBits>), grid, dim3(256), 0, stream, D, rows_each, digit_blocks, R);
     else if (D.np <= 8192)
-        hipLaunchKernelGGL((linear_digits_kernel<T, kPlanes, 4>), grid, dim3(256), 0, stream, D, rows_each);
+        hipLaunchKernelGGL((linear_prepare_kernel<T, kPlanes, 4, kBits>), grid, dim3(256), 0, stream, D, rows_each, digit_blocks, R);
     else
-        hipLaunchKernelGGL((linear_digits_kernel<T, kPlanes, 8>), grid, dim3(256), 0, stream, D, rows_each);
+        hipLaunchKernelGGL((linear_prepare_kernel<T, kPlanes, 8, kBits>), grid, dim3(256), 0, stream, D, rows_each, digit_blocks, R);
     return hipGetLastError();
 }
 
-hipError_t launch_transpose(const TransposeArgs &R, int bits, int experts, hipStream_t stream)
+template <typename T, int kPlanes>
+hipError_t prepare(const DigitArgs &D, const TransposeArgs &R, int bits, hipStream_t stream)
 {
-    if (R.k % 16 == 0 && (uintptr_t)R.w % (2 * bits) == 0 && R.ldw % (2 * bits) == 0) {
-        const dim3 grid((unsigned)((R.k + kTr - 1) / kTr), (unsigned)(R.np / kTr), (unsigned)experts);
-        if (bits == 8)
-            hipLaunchKernelGGL(linear_transpose_kernel<8>, grid, dim3(256), 0, stream, R);
-        else if (bits == 4)
-            hipLaunchKernelGGL(linear_transpose_kernel<4>, grid, dim3(256), 0, stream, R);
-        else
-            hipLaunchKernelGGL(linear_transpose_kernel<2>, grid, dim3(256), 0, stream, R);
-        return hipGetLastError();
+    const bool whole_rows = (uintptr_t)D.dy % 16 == 0 && D.ld_dy * sizeof(T) % 16 == 0 && D.n % 8 == 0 && (uintptr_t)D.ws % 16 == 0 && D.np <= 16384;
+    const bool whole_codes = R.k % 16 == 0 && (uintptr_t)R.w % (2 * bits) == 0 && R.ldw % (2 * bits) == 0;
+    const int64_t tiles = (int64_t)((R.k + kTr - 1) / kTr) * (R.np / kTr) * D.experts;
+    if (whole_rows && whole_codes && tiles < (int64_t)1 << 23) {
+        if (bits == 8) return launch_prepare<T, kPlanes, 8>(D, R, stream);
+        if (bits == 4) return launch_prepare<T, kPlanes, 4>(D, R, stream);
+        return launch_prepare<T, kPlanes, 2>(D, R, stream);
     }
-    const dim3 grid((unsigned)((R.k + 63) / 64), (unsigned)(R.np / 64), (unsigned)experts);
+    hipLaunchKernelGGL((linear_digits_any_kernel<T, kPlanes>), dim3((unsigned)(D.rows < 65536 ? D.rows : 65536)), dim3(256), 0, stream, D);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const dim3 grid((unsigned)((R.k + 63) / 64), (unsigned)(R.np / 64), (unsigned)D.experts);
     hipLaunchKernelGGL(linear_transpose_any_kernel, grid, dim3(256), 0, stream, R, bits);
     return hipGetLastError();
 }
@@ -339,10 +352,6 @@ hipError_t launch_linear_bwd(const void *dy, int64_t ld_dy, const void *w, int w
     D.np = np;
     D.experts = experts;
     D.ws_f16 = ws_f16;
-    hipError_t e = dtype == BQ_F32   ? launch_digits<float, 3>(D, stream)
-                   : dtype == BQ_F16 ? launch_digits<__half, 2>(D, stream)
-                                     : launch_digits<bf16_t, 2>(D, stream);
-    if (e != hipSuccess) return e;
     TransposeArgs R{};
     R.w = (const uint8_t *)w;
     R.out = (int8_t *)(base + L.weights);
@@ -352,7 +361,9 @@ hipError_t launch_linear_bwd(const void *dy, int64_t ld_dy, const void *w, int w
     R.n = n;
     R.k = k;
     R.np = np;
-    e = launch_transpose(R, wbits, experts, stream);
+    const hipError_t e = dtype == BQ_F32   ? prepare<float, 3>(D, R, wbits, stream)
+                         : dtype == BQ_F16 ? prepare<__half, 2>(D, R, wbits, stream)
+                                           : prepare<bf16_t, 2>(D, R, wbits, stream);
     if (e != hipSuccess) return e;
     LinearArgs A{};
     A.x = (const uint8_t *)(base + L.planes);

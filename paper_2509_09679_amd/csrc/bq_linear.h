@@ -151,7 +151,7 @@ int64_t linear_any_blocks(const LinearArgs &A);
 hipError_t launch_linear_rows8(const LinearArgs &A, int wbits, int planes, int blocks, int cols, hipStream_t stream);
 hipError_t launch_linear_rows4(const LinearArgs &A, int wbits, int blocks, int cols, hipStream_t stream);
 // many: bq_linear_tile.h
-enum LinearTile { kTileLarge, kTileMiddle, kTileSmall, kTileDeep };
+enum LinearTile { kTileLarge, kTileTall, kTileMiddle, kTileSmall, kTileDeep };
 hipError_t launch_linear_tile8(const LinearArgs &A, int wbits, LinearTile tile, hipStream_t stream);
 hipError_t launch_linear_tile4(const LinearArgs &A, int wbits, LinearTile tile, hipStream_t stream);
 hipError_t launch_linear_tile_digits(const LinearArgs &A, int planes, LinearTile tile, hipStream_t stream);

@@ -35,6 +35,7 @@ double pieces(const LinearArgs &A, int rows)
 //   128 x 128 deep 16    17    17    19    20    21    21    22    41    85   184
 //   128 x 128      23    24    24    26    26    27    28    26    36    70   147
 //   128 x 256      22    23    24    26    28    28    28    27    34    68   141
+//   192 x 256                                       41    42    37    42    84   139
 //   256 x 256      38    39    40    41    44    46    48    45    47    60   120
 
 // The weights' bytes, at what a kernel that has to wait for them reaches.
@@ -102,6 +103,7 @@ hipError_t launch_linear(const LinearArgs &A0, int xbits, int wbits, int planes,
         // 128 x 128: two workgroups on a compute unit, or one; packed codes have the same stages either way
         const bool packed = xbits < 8 || wbits < 8;
         tiles(kTileLarge, tile_us(A, wbits, planes, 256, 256, kCUs, 5.35, 1.50));
+        if (xbits == 8) tiles(kTileTall, tile_us(A, wbits, planes, 192, 256, kCUs, 4.3, 1.33));
         tiles(kTileMiddle, tile_us(A, wbits, planes, 128, 256, kCUs, 3.1, 0.93));
         tiles(kTileSmall, tile_us(A, wbits, planes, 128, 128, 2.0 * kCUs, 4.2, 0.93));
         tiles(packed ? kTileSmall : kTileDeep, tile_us(A, wbits, planes, 128, 128, kCUs, 4.4, 0.66));

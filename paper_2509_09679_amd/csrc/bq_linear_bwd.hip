@@ -158,9 +158,10 @@ __device__ __forceinline__ void digit_rows(const DigitArgs &A, int64_t block, in
 
 // Any rows; the second look at a row comes from the caches.
 template <typename T, int kPlanes>
-__global__ __launch_bounds__(256) void linear_digits_any_kernel(DigitArgs A)
+__device__ __forceinline__ void digit_rows_any(const DigitArgs &A, int64_t block, int rows_each)
 {
-    for (int64_t row = blockIdx.x; row < A.rows; row += gridDim.x) {
+    const int64_t end = (block + 1) * rows_each < A.rows ? (block + 1) * rows_each : A.rows;
+    for (int64_t row = block * rows_each; row < end; ++row) {
         const int expert = expert_of(A.offsets, A.experts, row);
         if (expert < 0) continue;
         const T *dy = (const T *)A.dy + row * A.ld_dy;
@@ -248,14 +249,17 @@ __device__ __forceinline__ void transpose_tile(const TransposeArgs &A, uint32_t 
     }
 }
 
-// Both in one launch: neither needs the other.  The first digit_blocks workgroups write digits, the others transpose.
+// Both in one launch: neither needs the other.  The first digit_blocks workgroups write digits (kPasses 0: of any rows), the others
+// transpose.
 template <typename T, int kPlanes, int kPasses, int kBits>
 __global__ __launch_bounds__(256) void linear_prepare_kernel(DigitArgs D, int rows_each, uint32_t digit_blocks, TransposeArgs R)
 {
-    if (blockIdx.x < digit_blocks)
-        digit_rows<T, kPlanes, kPasses>(D, blockIdx.x, rows_each);
-    else
+    if (blockIdx.x >= digit_blocks)
         transpose_tile<kBits>(R, blockIdx.x - digit_blocks);
+    else if constexpr (kPasses == 0)
+        digit_rows_any<T, kPlanes>(D, blockIdx.x, rows_each);
+    else
+        digit_rows<T, kPlanes, kPasses>(D, blockIdx.x, rows_each);
 }
 
 // The same for any width and alignment, 64 x 64 codes one by one.
@@ -282,13 +286,16 @@ __global__ __launch_bounds__(256) void linear_transpose_any_kernel(TransposeArgs
 int padded(int n) { return (n + 127) / 128 * 128; }
 
 template <typename T, int kPlanes, int kBits>
-hipError_t launch_prepare(const DigitArgs &D, const TransposeArgs &R, hipStream_t stream)
+hipError_t launch_prepare(const DigitArgs &D, const TransposeArgs &R, uint32_t transpose_blocks, hipStream_t stream)
 {
+    const bool whole = (uintptr_t)D.dy % 16 == 0 && D.ld_dy * sizeof(T) % 16 == 0 && D.n % 8 == 0 && (uintptr_t)D.ws % 16 == 0 && D.np <= 16384;
     // 8 workgroups fit a compute unit; beyond 4096 they take several rows each
     const int rows_each = (int)((D.rows + 4095) / 4096);
     const uint32_t digit_blocks = (uint32_t)((D.rows + rows_each - 1) / rows_each);
-    const dim3 grid(digit_blocks + (uint32_t)((R.k + kTr - 1) / kTr) * (uint32_t)(R.np / kTr) * (uint32_t)D.experts);
-    if (D.np <= 2048)
+    const dim3 grid(digit_blocks + transpose_blocks);
+    if (!whole)
+        hipLaunchKernelGGL((linear_prepare_kernel<T, kPlanes, 0, kBits>), grid, dim3(256), 0, stream, D, rows_each, digit_blocks, R);
+    else if (D.np <= 2048)
         hipLaunchKernelGGL((linear_prepare_kernel<T, kPlanes, 1, kBits>), grid, dim3(256), 0, stream, D, rows_each, digit_blocks, R);
     else if (D.np <= 4096)
         hipLaunchKernelGGL((linear_prepare_kernel<T, kPlanes, 2, kBits>), grid, dim3(256), 0, stream, D, rows_each, digit_blocks, R);
@@ -302,16 +309,13 @@ hipError_t launch_prepare(const DigitArgs &D, const TransposeArgs &R, hipStream_
 template <typename T, int kPlanes>
 hipError_t prepare(const DigitArgs &D, const TransposeArgs &R, int bits, hipStream_t stream)
 {
-    const bool whole_rows = (uintptr_t)D.dy % 16 == 0 && D.ld_dy * sizeof(T) % 16 == 0 && D.n % 8 == 0 && (uintptr_t)D.ws % 16 == 0 && D.np <= 16384;
-    const bool whole_codes = R.k % 16 == 0 && (uintptr_t)R.w % (2 * bits) == 0 && R.ldw % (2 * bits) == 0;
     const int64_t tiles = (int64_t)((R.k + kTr - 1) / kTr) * (R.np / kTr) * D.experts;
-    if (whole_rows && whole_codes && tiles < (int64_t)1 << 23) {
-        if (bits == 8) return launch_prepare<T, kPlanes, 8>(D, R, stream);
-        if (bits == 4) return launch_prepare<T, kPlanes, 4>(D, R, stream);
-        return launch_prepare<T, kPlanes, 2>(D, R, stream);
+    if (R.k % 16 == 0 && (uintptr_t)R.w % (2 * bits) == 0 && R.ldw % (2 * bits) == 0 && tiles < (int64_t)1 << 23) {
+        if (bits == 8) return launch_prepare<T, kPlanes, 8>(D, R, (uint32_t)tiles, stream);
+        if (bits == 4) return launch_prepare<T, kPlanes, 4>(D, R, (uint32_t)tiles, stream);
+        return launch_prepare<T, kPlanes, 2>(D, R, (uint32_t)tiles, stream);
     }
-    hipLaunchKernelGGL((linear_digits_any_kernel<T, kPlanes>), dim3((unsigned)(D.rows < 65536 ? D.rows : 65536)), dim3(256), 0, stream, D);
-    hipError_t e = hipGetLastError();
+    const hipError_t e = launch_prepare<T, kPlanes, 8>(D, R, 0, stream);
     if (e != hipSuccess) return e;
     const dim3 grid((unsigned)((R.k + 63) / 64), (unsigned)(R.np / 64), (unsigned)D.experts);
     hipLaunchKernelGGL(linear_transpose_any_kernel, grid, dim3(256), 0, stream, R, bits);

@@ -294,6 +294,7 @@ hipError_t launch_tile(const LinearArgs &A, hipStream_t stream)
 
 // x rows (tokens times planes) x channels
 typedef TileShape<2, 4, 8, 160> TileLarge;   // 256 x 256
+typedef TileShape<2, 4, 6, 160> TileTall;    // 192 x 256, for 8-bit codes
 typedef TileShape<2, 4, 4, 160> TileMiddle;  // 128 x 256
 typedef TileShape<2, 2, 4, 80> TileSmall;    // 128 x 128, two workgroups per compute unit
 typedef TileShape<2, 2, 4, 160> TileDeep;    // 128 x 128, one of them with all of the LDS (8-bit codes: four stages instead of two)

@@ -7,6 +7,7 @@ template <int kWBits>
 static hipError_t launch(const LinearArgs &A, LinearTile tile, hipStream_t stream)
 {
     if (tile == kTileLarge) return launch_tile<8, kWBits, 1, TileLarge>(A, stream);
+    if (tile == kTileTall) return launch_tile<8, kWBits, 1, TileTall>(A, stream);
     if (tile == kTileMiddle) return launch_tile<8, kWBits, 1, TileMiddle>(A, stream);
     if constexpr (kWBits == 8) {
         if (tile == kTileDeep) return launch_tile<8, 8, 1, TileDeep>(A, stream);

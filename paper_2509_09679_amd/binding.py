@@ -429,45 +429,63 @@ def bq_linear_bwd_workspace_bytes(desc: bq_linear) -> int:
 
 
 def _needs(d: bq_linear):
-    """What the tensors of a call have to have: the types of codes, scales and values; how many rows, and elements of x, scales per
-    channel, w, y (or dy) and dx; the row strides of x (or dx), w and y (or dy)."""
+    """What the tensors of a call have to have: the types of codes, scales and values; how many rows and scales per channel; shape and
+    strides of x, of w as one matrix or one per expert, of y (or dy) and of dx."""
     per_channel = d.experts * d.outputs
-    needs = (_torch_types(-1), (_torch_types(d.scale_dtype) or (None,))[0], (_torch_types(d.dtype) or (None,))[0], d.rows,
-             (d.inputs * d.xbits + 7) // 8 * d.rows, per_channel, (d.inputs * d.wbits + 7) // 8 * per_channel, d.rows * d.outputs,
-             d.rows * d.inputs, d.ld_x, d.ld_w, d.ld_y)
+    x_width, w_width = (d.inputs * d.xbits + 7) // 8, (d.inputs * d.wbits + 7) // 8
+    needs = (_torch_types(-1), (_torch_types(d.scale_dtype) or (None,))[0], (_torch_types(d.dtype) or (None,))[0], d.rows, per_channel,
+             ((d.rows, x_width), (d.ld_x, 1)),
+             {(per_channel, w_width): (d.ld_w, 1), (d.experts, d.outputs, w_width): (d.ld_w * d.outputs, d.ld_w, 1)},
+             ((d.rows, d.outputs), (d.ld_y, 1)), ((d.rows, d.inputs), (d.ld_x, 1)))
     d.__dict__["needs"] = needs
     return needs
 
 
-def _require_strides(who: str, tensors) -> None:
-    """tensors: (name, tensor, the row stride that the descriptor says)."""
-    for name, t, ld in tensors:
-        if t is not None and t.dim() >= 2 and t.shape[-2] > 1:
-            _require(t.stride(-2) == ld, 2, f"{who}: rows of {name} are {t.stride(-2)} elements apart, the descriptor says {ld}")
+def _refuse_layouts(who: str, tensors) -> None:
+    """tensors: (name, tensor, {the shapes that the descriptor says: their strides}); strides of dimensions of one element do not matter."""
+    for name, t, layouts in tensors:
+        if t is None:
+            continue
+        shape, strides = tuple(t.shape), t.stride()
+        _require(shape in layouts, 2, f"{who}: {name} has the shape {list(shape)}, the descriptor says {[list(s) for s in layouts]}")
+        for size, has, says, what in zip(shape[::-1], strides[::-1], layouts[shape][::-1], ("elements", "rows", "experts")):
+            _require(size == 1 or has == says or t.numel() == 0, 2,
+                     f"{who}: {what} of {name} are {has} elements apart, the descriptor says {says}")
 
 
 def _check_fwd(who: str, d: bq_linear, x, xscale, w, wscale, bias, y) -> None:
-    codes, scale, value, rows, n_x, channels, n_w, n_y, _, ld_x, ld_w, ld_y = d.__dict__.get("needs") or _needs(d)
+    codes, scale, value, rows, channels, x_is, w_is, y_is, _ = d.__dict__.get("needs") or _needs(d)
     here = _here()
     if (x is not None and w is not None and xscale is not None and wscale is not None and y is not None
             and x.get_device() == w.get_device() == xscale.get_device() == wscale.get_device() == y.get_device() == here
-            and x.dtype in codes and w.dtype in codes and xscale.dtype is wscale.dtype is scale and y.dtype is value and x.numel() >= n_x
-            and w.numel() >= n_w and y.numel() >= n_y and xscale.numel() >= rows and wscale.numel() >= channels and xscale.is_contiguous()
-            and wscale.is_contiguous() and bias is None and w.stride(-2) == ld_w and (rows <= 1 or (x.stride(0) == ld_x and y.stride(0) == ld_y))):
+            and x.dtype in codes and w.dtype in codes and xscale.dtype is wscale.dtype is scale and y.dtype is value
+            and (x.shape, x.stride()) == x_is and w.stride() == w_is.get(w.shape) and (y.shape, y.stride()) == y_is
+            and xscale.numel() >= rows and wscale.numel() >= channels and xscale.is_contiguous() and wscale.is_contiguous()
+            and (bias is None or (bias.get_device() == here and bias.dtype is value and bias.numel() >= channels and bias.is_contiguous()))):
         return
-    _refuse_tensors(who, (("x", x, codes, n_x, False), ("xscale", xscale, (scale,), rows, True), ("w", w, codes, n_w, False),
-                          ("wscale", wscale, (scale,), channels, True), ("bias", bias, (value,), channels, True), ("y", y, (value,), n_y, False)))
-    _require_strides(who, (("x", x, ld_x), ("w", w, ld_w), ("y", y, ld_y)))
+    _refuse_tensors(who, (("x", x, codes, 0, False), ("xscale", xscale, (scale,), rows, True), ("w", w, codes, 0, False),
+                          ("wscale", wscale, (scale,), channels, True), ("bias", bias, (value,), channels, True), ("y", y, (value,), 0, False)))
+    _refuse_layouts(who, (("x", x, dict([x_is])), ("w", w, w_is), ("y", y, dict([y_is]))))
 
 
 def _check_bwd(who: str, d: bq_linear, dy, w, wscale, dx, workspace) -> None:
-    codes, scale, value, _, _, channels, n_w, n_y, n_dx, ld_x, ld_w, ld_y = d.__dict__.get("needs") or _needs(d)
-    _refuse_tensors(who, (("dy", dy, (value,), n_y, False), ("w", w, codes, n_w, False), ("wscale", wscale, (scale,), channels, True),
-                          ("dx", dx, (value,), n_dx, False), ("workspace", workspace, _torch_types(-3), 0, True)))
-    _require_strides(who, (("dy", dy, ld_y), ("w", w, ld_w), ("dx", dx, ld_x)))
+    codes, scale, value, _, channels, _, w_is, y_is, dx_is = d.__dict__.get("needs") or _needs(d)
+    here = _here()
+    if (dy is not None and w is not None and wscale is not None and dx is not None and workspace is not None
+            and dy.get_device() == w.get_device() == wscale.get_device() == dx.get_device() == workspace.get_device() == here
+            and w.dtype in codes and wscale.dtype is scale and dy.dtype is dx.dtype is value and workspace.dtype in _torch_types(-3)
+            and (dy.shape, dy.stride()) == y_is and w.stride() == w_is.get(w.shape) and (dx.shape, dx.stride()) == dx_is
+            and wscale.numel() >= channels and wscale.is_contiguous() and workspace.is_contiguous()):
+        return
+    _refuse_tensors(who, (("dy", dy, (value,), 0, False), ("w", w, codes, 0, False), ("wscale", wscale, (scale,), channels, True),
+                          ("dx", dx, (value,), 0, False), ("workspace", workspace, _torch_types(-3), 0, True)))
+    _refuse_layouts(who, (("dy", dy, dict([y_is])), ("w", w, w_is), ("dx", dx, dict([dx_is]))))
 
 
 def _check_offsets(who: str, d: bq_linear, offsets) -> None:
+    if (offsets is not None and offsets.dtype in _torch_types(-2) and offsets.get_device() == _here() and offsets.numel() > d.experts
+            and offsets.is_contiguous()):
+        return
     _refuse_tensors(who, (("offsets", offsets, _torch_types(-2), d.experts + 1, True),))
 
 

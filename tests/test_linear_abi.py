@@ -164,3 +164,34 @@ def test_tensors_the_library_cannot_see(monkeypatch):
     monkeypatch.setattr(B, "_here", lambda: 0)  # tensors of another device
     with pytest.raises(B.BqError, match="current device"):
         fwd()
+
+
+def test_tensors_laid_out_otherwise_than_the_descriptor(monkeypatch):
+    # all of these have the elements that the call needs, and would be read at the wrong places or behind their ends
+    monkeypatch.setattr(B, "_here", lambda: -1)
+    codes = lambda *s: torch.zeros(*s, dtype=torch.int8)  # noqa: E731
+    x, w, ws, y, xs, off = codes(6, 32), codes(3, 4, 32), torch.zeros(3, 4), torch.zeros(6, 4), torch.zeros(6), torch.zeros(4, dtype=torch.int32)
+    dx, work = torch.zeros(6, 32), torch.zeros(10, dtype=torch.uint8)
+    wide = codes(6, 64)
+    d, g = B.make_linear(x, w, ws, y), B.make_linear_bwd(y, w, ws, dx)
+    p = B.make_linear(wide[:, :32], w, ws, y)  # rows of 32 that are 64 apart
+
+    def fwd(x=x, w=w, b=None, y=y, d=d):
+        B.bq_linear_grouped_fwd(x, xs, w, ws, b, off, y, d)
+
+    def bwd(dy=y, w=w, dx=dx):
+        B.bq_linear_grouped_bwd(dy, w, ws, off, dx, work, g)
+
+    for call in (lambda: fwd(x=wide[:, ::2], d=p), lambda: fwd(x=wide[:3], d=p), lambda: fwd(x=x.reshape(-1), d=d), lambda: fwd(x=x.reshape(3, 64)),
+                 lambda: fwd(w=codes(6, 4, 32)[::2]), lambda: fwd(w=codes(3, 32, 4).transpose(1, 2)), lambda: fwd(w=w.reshape(4, 3, 32)),
+                 lambda: fwd(y=torch.zeros(4, 6).t()), lambda: fwd(b=torch.zeros(3, 8)[:, ::2]), lambda: bwd(dy=torch.zeros(6, 8)[:, ::2]),
+                 lambda: bwd(w=codes(6, 4, 32)[1::2]), lambda: bwd(dx=torch.zeros(32, 6).t()), lambda: bwd(dx=dx.reshape(12, 16))):
+        with pytest.raises(B.BqError) as e:
+            call()
+        assert e.value.status == 2, str(e.value)
+    # strides of dimensions of one element do not matter, and the experts' weights may be one matrix
+    one = B.make_linear(x[:1], w[:1, :1], ws[:1, :1], y[:1, :1])
+    B._check_fwd("t", one, x[:1], xs, w[2:, 3:], ws[:1, :1], None, y[3:4, 2:3])
+    B._check_fwd("t", p, wide[:, 32:], xs, w.reshape(12, 32), ws, torch.zeros(12), y)
+    B._check_bwd("t", g, y, w.reshape(12, 32), ws, dx, work)
+    B._check_bwd("t", g, y, w, ws, dx, work)

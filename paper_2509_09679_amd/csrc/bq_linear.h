@@ -145,7 +145,7 @@ __device__ __forceinline__ void store_row_value(void *p, int64_t at, int dtype, 
 }
 
 // ---- launchers --------------------------------------------------------------------------------------------
-hipError_t launch_linear_any(const LinearArgs &A, int xbits, int wbits, int planes, hipStream_t stream);  // bq_linear_any.hip
+hipError_t launch_linear_any(const LinearArgs &A, int xbits, int wbits, hipStream_t stream);  // bq_linear_any.hip
 int64_t linear_any_blocks(const LinearArgs &A);
 // few rows: bq_linear_rows.h; blocks x cols: 16-token blocks and 16-channel columns of a workgroup
 hipError_t launch_linear_rows8(const LinearArgs &A, int wbits, int planes, int blocks, int cols, hipStream_t stream);

@@ -71,7 +71,7 @@ hipError_t launch_linear(const LinearArgs &A0, int xbits, int wbits, int planes,
     A.factor /= (float)((1 << (8 - xbits)) * (1 << (8 - wbits)));
     const size_t size = A.dtype == BQ_F32 ? 4 : 2;
     A.y_quads = (uintptr_t)A.y % 16 == 0 && A.ldy * size % 16 == 0;
-    if (!fast_layout(A, xbits, wbits)) return launch_linear_any(A, xbits, wbits, planes, stream);
+    if (!fast_layout(A, xbits, wbits)) return launch_linear_any(A, xbits, wbits, stream);
 
     int blocks = 1, cols = 1;
     LinearTile tile = kTileLarge;

@@ -1,5 +1,6 @@
 // The product for any width, stride and alignment: a workgroup of four waves takes 64 tokens x 64 channels, its threads fetch the
-// codes one by one and lay them out as bytes in LDS.  Bound by those loads; the shapes of real layers go to the other kernels.
+// codes one by one and lay them out as bytes in LDS.  Bound by those loads; the shapes of real layers go to the other kernels, and so do
+// all digits of gradients, whose rows are padded.
 #include "bq_linear.h"
 
 namespace bq {
@@ -15,7 +16,6 @@ __device__ __forceinline__ uint8_t code_at(const uint8_t *row, int k, int bits)
     return (uint8_t)((row[k >> 2] >> ((k & 3) * 2)) << 6);
 }
 
-template <int kPlanes>
 __global__ __launch_bounds__(256) void linear_any_kernel(LinearArgs A, int xbits, int wbits)
 {
     __shared__ __align__(16) uint8_t s_x[kTile * kLd], s_w[kTile * kLd];
@@ -29,38 +29,27 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinearArgs A, int xbits
     const int srow = tid >> 2, sk = (tid & 3) * 16;  // the 16 codes this thread fetches
     const int64_t token = rt.row0 + srow;
     const bool has_token = token < rt.row_end, has_channel = o0 + srow < A.n;
-    const uint8_t *wrow = A.w + rt.expert * A.w_step + (int64_t)(o0 + srow) * A.ldw;
-    int64_t total[2][2][4] = {};
+    const uint8_t *wrow = A.w + rt.expert * A.w_step + (int64_t)(o0 + srow) * A.ldw, *xrow = A.x + token * A.ldx;
+    i32x4 acc[2][2] = {};
+    for (int k0 = 0; k0 < A.k; k0 += kStep) {
+        __syncthreads();
 #pragma unroll
-    for (int p = 0; p < kPlanes; ++p) {
-        const uint8_t *xrow = A.x + p * A.plane_step + token * A.ldx;
-        i32x4 acc[2][2] = {};
-        for (int k0 = 0; k0 < A.k; k0 += kStep) {
-            __syncthreads();
+        for (int j = 0; j < 16; ++j) {
+            const int k = k0 + sk + j;
+            s_x[srow * kLd + sk + j] = has_token && k < A.k ? code_at(xrow, k, xbits) : 0;
+            s_w[srow * kLd + sk + j] = has_channel && k < A.k ? code_at(wrow, k, wbits) : 0;
+        }
+        __syncthreads();
+        i32x4 w[2], x[2];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const int k = k0 + sk + j;
-                s_x[srow * kLd + sk + j] = has_token && k < A.k ? code_at(xrow, k, xbits) : 0;
-                s_w[srow * kLd + sk + j] = has_channel && k < A.k ? code_at(wrow, k, wbits) : 0;
-            }
-            __syncthreads();
-            i32x4 w[2], x[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                w[i] = *(const i32x4 *)(s_w + (to + 16 * i + r16) * kLd + kq);
-                x[i] = *(const i32x4 *)(s_x + (tt + 16 * i + r16) * kLd + kq);
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i], x[j], acc[i][j], 0, 0, 0);
+        for (int i = 0; i < 2; ++i) {
+            w[i] = *(const i32x4 *)(s_w + (to + 16 * i + r16) * kLd + kq);
+            x[i] = *(const i32x4 *)(s_x + (tt + 16 * i + r16) * kLd + kq);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) total[i][j][r] = total[i][j][r] * 256 + acc[i][j][r];
+            for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i], x[j], acc[i][j], 0, 0, 0);
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -74,8 +63,7 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinearArgs A, int xbits
                 const int o = o0 + to + 16 * i + (lane >> 4) * 4 + r;
                 if (o >= A.n) continue;
                 const int64_t at = (int64_t)rt.expert * A.n + o;
-                float v = (float)total[i][j][r] * xs;
-                if (A.ws) v *= load_scale(A.ws, at, A.ws_f16);
+                float v = (float)acc[i][j][r] * xs * load_scale(A.ws, at, A.ws_f16);
                 if (A.bias) v += load_row_value(A.bias, at, A.dtype);
                 store_row_value(A.y, t * A.ldy + o, A.dtype, v);
             }
@@ -86,15 +74,9 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinearArgs A, int xbits
 
 int64_t linear_any_blocks(const LinearArgs &A) { return row_tiles_bound(A, kTile) * ((A.n + kTile - 1) / kTile); }
 
-hipError_t launch_linear_any(const LinearArgs &A, int xbits, int wbits, int planes, hipStream_t stream)
+hipError_t launch_linear_any(const LinearArgs &A, int xbits, int wbits, hipStream_t stream)
 {
-    const dim3 grid((unsigned)linear_any_blocks(A));
-    if (planes == 1)
-        hipLaunchKernelGGL(linear_any_kernel<1>, grid, dim3(256), 0, stream, A, xbits, wbits);
-    else if (planes == 2)
-        hipLaunchKernelGGL(linear_any_kernel<2>, grid, dim3(256), 0, stream, A, xbits, wbits);
-    else
-        hipLaunchKernelGGL(linear_any_kernel<3>, grid, dim3(256), 0, stream, A, xbits, wbits);
+    hipLaunchKernelGGL(linear_any_kernel, dim3((unsigned)linear_any_blocks(A)), dim3(256), 0, stream, A, xbits, wbits);
     return hipGetLastError();
 }
 

@@ -407,3 +407,87 @@ def test_rows_quant8_of_more_rows_than_workgroups(rows, cols):
         s = (v.abs().amax(1).double() / 127.0).float()
         assert torch.equal(scales[a:a + (1 << 19)], s)
         assert torch.equal(codes[a:a + (1 << 19)], torch.round(v * (1.0 / s.double()).float()[:, None]).clamp_(-128, 127).to(torch.int8))
+
+
+# ---- every kernel that a product may take: batches of every size, odd numbers of tokens and channels, a short last step ----------------
+
+
+def _ragged(T, experts):
+    """Experts of uneven sizes, some empty, and rows of none at both ends."""
+    cuts = np.sort(np.random.default_rng([T, experts]).integers(min(1, T), T + 1, size=experts + 1))
+    cuts[experts // 2] = cuts[experts // 2 + 1]
+    return [int(c) for c in cuts]
+
+
+BATCHES_FWD = [(1, 18, 64, 0), (3, 1500, 64, 3), (115, 520, 64, 0), (200, 650, 64, 0), (830, 140, 64, 3), (45, 200, 64, 50), (500, 1000, 64, 0), (150, 200, 64, 3),
+               (115, 2050, 64, 0), (450, 2050, 64, 0), (187, 520, 64, 3), (115, 1500, 64, 3), (115, 4100, 64, 0), (380, 330, 64, 0), (390, 4100, 832, 0),
+               (200, 20000, 64, 3), (300, 20000, 64, 3), (4100, 2050, 64, 50), (4096, 16, 64, 64)]
+BATCHES_BWD = [(1, 18, 0), (150, 200, 3), (200, 330, 0), (200, 300, 3), (700, 200, 0), (600, 200, 0), (830, 780, 0), (450, 520, 0), (390, 650, 0),
+               (420, 1500, 0), (4100, 520, 50), (600, 6000, 3), (4100, 780, 50), (4096, 16, 64)]
+
+
+@pytest.mark.parametrize("xbits,wbits", BITS)
+@pytest.mark.parametrize("T,N,K,experts", BATCHES_FWD)
+def test_batches_fwd(T, N, K, experts, xbits, wbits):
+    gen = torch.Generator(device=DEV).manual_seed(T + N)
+    E, offsets = max(1, experts), _ragged(T, experts) if experts else [0, T]
+    qx, x = _codes_on_device(gen, (T, K), xbits)
+    qw, w = _codes_on_device(gen, (E, N, K), wbits)
+    xs, ws = (torch.rand(s, generator=gen, device=DEV) * 0.01 + 1e-3 for s in ((T,), (E, N)))
+    b = torch.randn((E, N), generator=gen, device=DEV)
+    y = torch.full((T, N), 3.0, device=DEV)
+    if experts:
+        B.bq_linear_grouped_fwd(x, xs, w, ws, b, lu.offsets_tensor(offsets), y, B.make_linear(x, w, ws, y, xbits=xbits, wbits=wbits))
+    else:
+        B.bq_linear_fwd(x, xs, w[0], ws[0], b[0], y, B.make_linear(x, w[0], ws[0], y, xbits=xbits, wbits=wbits))
+    for e in range(E):
+        lo, hi = offsets[e], offsets[e + 1]
+        p = (qx[lo:hi] @ qw[e].t()) * xs[lo:hi, None].double() * ws[e].double()
+        _within(y[lo:hi], p + b[e].double(), 5 * 2.0 ** -24 * (p.abs() + b[e].double().abs()) + 1e-40)
+    assert (y[:offsets[0]] == 3).all() and (y[offsets[-1]:] == 3).all()
+
+
+def _check_bwd(T, N, K, experts, wbits, dtype, scale, seed):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    E, offsets = max(1, experts), _ragged(T, experts) if experts else [0, T]
+    qw, w = _codes_on_device(gen, (E, N, K), wbits)
+    ws = (torch.rand((E, N), generator=gen, device=DEV) * 0.01 + 1e-3).to(TORCH[scale])
+    dy = (torch.randn((T, N), generator=gen, device=DEV) * torch.exp(torch.randn((T, 1), generator=gen, device=DEV))).to(TORCH[dtype])
+    dx = torch.full((T, K), 3.0, dtype=TORCH[dtype], device=DEV)
+    wd, wsd = (w, ws) if experts else (w[0], ws[0])
+    d = B.make_linear_bwd(dy, wd, wsd, dx, wbits=wbits)
+    work = torch.full((B.bq_linear_bwd_workspace_bytes(d),), 0xA5, dtype=torch.uint8, device=DEV)
+    if experts:
+        B.bq_linear_grouped_bwd(dy, wd, wsd, lu.offsets_tensor(offsets), dx, work, d)
+    else:
+        B.bq_linear_bwd(dy, wd, wsd, dx, work, d)
+    term = 0.5 / lu.QMAX[3 if dtype == "f32" else 2] + 5 * 2.0 ** -24
+    for e in range(E):
+        lo, hi = offsets[e], offsets[e + 1]
+        if lo == hi:
+            continue
+        v = dy[lo:hi].double() * ws[e].double()
+        want = v @ qw[e]
+        f32 = term * v.abs().amax(1, keepdim=True) * qw[e].abs().sum(0) + 2 * 2.0 ** -24 * want.abs()
+        _within(dx[lo:hi], want, f32 + (lu.half_step(dtype) * (want.abs() + f32) + lu.smallest(dtype) if dtype != "f32" else 0) + 1e-40)
+    assert (dx[:offsets[0]] == 3).all() and (dx[offsets[-1]:] == 3).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("T,K,experts", BATCHES_BWD)
+def test_batches_bwd(T, K, experts, dtype):
+    _check_bwd(T, 640 if K == 1500 else 72, K, experts, 8, dtype, "f32", T + K)
+
+
+@pytest.mark.parametrize("wbits", [8, 4, 2])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("N", [104, 2048, 2056, 4104, 8200, 16384, 16392, 1001])
+def test_bwd_of_wide_layers(N, dtype, wbits):
+    # rows of digits from one piece of a workgroup to the widest that stay in registers, and those that do not
+    _check_bwd(5, N, 48, 0, wbits, dtype, "f16" if N % 3 else "f32", N)
+    _check_bwd(37, N, 80, 4, wbits, dtype, "f32" if N % 3 else "f16", N + 1)
+
+
+def test_bwd_of_more_rows_than_workgroups():
+    _check_bwd(4096 * 2 + 77, 256, 64, 0, 8, "bf16", "f32", 1)
+    _check_bwd(4096 * 2 + 77, 250, 64, 3, 4, "f16", "f32", 2)

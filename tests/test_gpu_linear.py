@@ -491,3 +491,68 @@ def test_bwd_of_wide_layers(N, dtype, wbits):
 def test_bwd_of_more_rows_than_workgroups():
     _check_bwd(4096 * 2 + 77, 256, 64, 0, 8, "bf16", "f32", 1)
     _check_bwd(4096 * 2 + 77, 250, 64, 3, 4, "f16", "f32", 2)
+
+
+# ---- places beyond 2^32 ---------------------------------------------------------------------------------
+
+
+def _spread(a, ld):
+    """A device tensor with a's values whose rows lie ld elements apart."""
+    buf = torch.empty((a.shape[0] - 1) * ld + a.shape[1], dtype=a.dtype, device=DEV)
+    v = buf.as_strided(a.shape, (ld, 1))
+    v.copy_(a)
+    return v
+
+
+def test_rows_quant8_beyond_32_bits():
+    a = torch.randn(6, 520, device=DEV, generator=torch.Generator(device=DEV).manual_seed(1))
+    want, scales = B.alloc_rows_quant8(6, 520, "f32", DEV)
+    B.bq_rows_quant8(a, want, scales)
+    x, codes, got = _spread(a, (1 << 30) - 24), _spread(torch.zeros_like(want), (1 << 30) - 8), torch.empty_like(scales)
+    B.bq_rows_quant8(x, codes, got)
+    assert torch.equal(codes, want) and torch.equal(got, scales)
+
+
+@pytest.mark.parametrize("bits", [(8, 8), (4, 2)])
+@pytest.mark.parametrize("T,N,ld_x,ld_w,ld_y", [(1100, 40, 1 << 22, 64, 64), (1300, 2200, 1 << 22, 1 << 21, 1 << 21), (40, 1500, 64, 1 << 22, 1 << 21),
+                                                (6, 5, 1 << 30, 64, 1 << 29), (6, 5, 64, 1 << 30, 8)])
+def test_linear_fwd_beyond_32_bits(T, N, ld_x, ld_w, ld_y, bits):
+    L = Layer(np.random.default_rng([T, N]), T, N, 64, xbits=bits[0], wbits=bits[1], dtype="f32", bias=True)
+    want, size = lu.reference_fwd(L.qx, L.xs, L.qw, L.ws, L.bias, [0, T])
+    L.x, L.w = _spread(L.x, ld_x), _spread(L.w, ld_w)
+    y = _spread(torch.full((T, N), 3.0, device=DEV), ld_y)
+    B.bq_linear_fwd(L.x, L.xs, L.w, L.ws, L.bias, y, B.make_linear(L.x, L.w, L.ws, y, xbits=bits[0], wbits=bits[1], inputs=64))
+    lu.check(lu.f64(y), want, lu.bound_fwd(want, size, "f32"), f"{bits}")
+
+
+@pytest.mark.parametrize("T,N,K,ld_y,ld_x", [(9, 200, 48, 1 << 30, 1 << 29), (1100, 136, 96, 1 << 22, 1 << 21)])
+def test_linear_bwd_rows_beyond_32_bits(T, N, K, ld_y, ld_x):
+    rng = np.random.default_rng([T, N, K])
+    L = Layer(rng, T, N, K, dtype="bf16")
+    dy = _gradient(rng, T, N, "bf16")
+    want, weight, top = lu.reference_bwd(dy, L.qw, L.ws, [0, T])
+    dy, dx = _spread(dy, ld_y), _spread(torch.full((T, K), 3.0, dtype=torch.bfloat16, device=DEV), ld_x)
+    d = B.make_linear_bwd(dy, L.w, L.ws, dx)
+    B.bq_linear_bwd(dy, L.w, L.ws, dx, torch.empty(B.bq_linear_bwd_workspace_bytes(d), dtype=torch.uint8, device=DEV), d)
+    lu.check(lu.f64(dx), want, lu.bound_bwd(want, weight, top, "bf16"), "dx")
+
+
+def test_linear_bwd_workspace_beyond_32_bits():
+    # the digits of 600000 rows of 4096, then 70 experts whose transposed weights fill 4.7 GB, of which two have rows
+    _check_bwd(600000, 4096, 64, 0, 4, "bf16", "f32", 5)
+    E, N, K, T = 70, 8192, 8192, 24
+    gen = torch.Generator(device=DEV).manual_seed(6)
+    w = torch.randint(-128, 128, (E, N, K), generator=gen, device=DEV, dtype=torch.int8)
+    ws = torch.rand((E, N), generator=gen, device=DEV) * 0.01 + 1e-3
+    dy = torch.randn((T, N), generator=gen, device=DEV).bfloat16()
+    offsets = [0] + [9] * 68 + [9, T]
+    dx = torch.full((T, K), 3.0, dtype=torch.bfloat16, device=DEV)
+    d = B.make_linear_bwd(dy, w, ws, dx)
+    assert B.bq_linear_bwd_workspace_bytes(d) > 1 << 32
+    work = torch.empty(B.bq_linear_bwd_workspace_bytes(d), dtype=torch.uint8, device=DEV)
+    B.bq_linear_grouped_bwd(dy, w, ws, lu.offsets_tensor(offsets), dx, work, d)
+    for e, lo, hi in ((0, 0, 9), (E - 1, 9, T)):
+        v, q = dy[lo:hi].double() * ws[e].double(), w[e].double()
+        want = v @ q
+        f32 = (0.5 / lu.QMAX[2] + 5 * 2.0 ** -24) * v.abs().amax(1, keepdim=True) * q.abs().sum(0) + 2 * 2.0 ** -24 * want.abs()
+        _within(dx[lo:hi], want, f32 + lu.half_step("bf16") * (want.abs() + f32) + 1e-40)

@@ -31,6 +31,7 @@ struct LinearArgs {
     int xs_f16, ws_f16, dtype;
     float factor;  // of the fields' positions
     int y_quads;   // rows of y are 16-byte aligned
+    int w_rows;    // of weights that lie across (bq_linear_tile.h): the summed index may be padded beyond it
 };
 
 // Rows of one expert that a workgroup takes: [row0, row_end), at most the tile's.
@@ -155,7 +156,11 @@ enum LinearTile { kTileLarge, kTileTall, kTileMiddle, kTileSmall, kTileDeep };
 hipError_t launch_linear_tile8(const LinearArgs &A, int wbits, LinearTile tile, hipStream_t stream);
 hipError_t launch_linear_tile4(const LinearArgs &A, int wbits, LinearTile tile, hipStream_t stream);
 hipError_t launch_linear_tile_digits(const LinearArgs &A, int planes, LinearTile tile, hipStream_t stream);
+hipError_t launch_linear_tile_across(const LinearArgs &A, int wbits, int planes, LinearTile tile, hipStream_t stream);
 // picks the kernel; planes: 1 for codes, 2 or 3 for a gradient's digits (bq_linear.hip)
 hipError_t launch_linear(const LinearArgs &A, int xbits, int wbits, int planes, hipStream_t stream);
+// the gradient's product with the weights as the layer has them, [summed index][channel]; is it quicker than transposing them first?
+bool linear_across_is_quicker(const LinearArgs &across, const LinearArgs &turned, int wbits, int planes);
+hipError_t launch_linear_across(const LinearArgs &A, int wbits, int planes, hipStream_t stream);
 
 }  // namespace bq

@@ -9,6 +9,13 @@ namespace {
 
 constexpr double kCUs = 256.0;
 
+struct Choice {
+    double us;
+    bool few;
+    int blocks, cols;
+    LinearTile tile;
+};
+
 bool fast_layout(const LinearArgs &A, int xbits, int wbits)
 {
     // whole 16-byte pieces of both operands; offsets within a tile of 256 rows in 32 bits
@@ -63,41 +70,25 @@ double tile_us(const LinearArgs &A, int wbits, int planes, int x_rows, int chann
     return 2.15 + (codes > weights ? codes : weights);
 }
 
-}  // namespace
-
-hipError_t launch_linear(const LinearArgs &A0, int xbits, int wbits, int planes, hipStream_t stream)
+Choice choose(const LinearArgs &A, int xbits, int wbits, int planes, bool across)
 {
-    LinearArgs A = A0;
-    A.factor /= (float)((1 << (8 - xbits)) * (1 << (8 - wbits)));
-    const size_t size = A.dtype == BQ_F32 ? 4 : 2;
-    A.y_quads = (uintptr_t)A.y % 16 == 0 && A.ldy * size % 16 == 0;
-    if (!fast_layout(A, xbits, wbits)) return launch_linear_any(A, xbits, wbits, stream);
-
-    int blocks = 1, cols = 1;
-    LinearTile tile = kTileLarge;
-    bool few = true;
-    double best = rows_us(A, xbits, wbits, planes, 1, 1);
-    auto rows = [&](int b, int c) {
-        const double us = rows_us(A, xbits, wbits, planes, b, c);
-        if (us < best) {
-            best = us;
-            blocks = b;
-            cols = c;
-        }
+    Choice c{1e30, true, 1, 1, kTileLarge};
+    auto rows = [&](int b, int n) {
+        const double us = rows_us(A, xbits, wbits, planes, b, n);
+        if (us < c.us) c = Choice{us, true, b, n, kTileLarge};
     };
     auto tiles = [&](LinearTile which, double us) {
-        if (us < best) {
-            best = us;
-            few = false;
-            tile = which;
-        }
+        if (us < c.us) c = Choice{us, false, 0, 0, which};
     };
-    rows(1, 2);
-    rows(2, 1);
-    if (planes < 3) rows(2, 2);
-    if (planes == 1) {
-        rows(1, 4);
-        rows(4, 2);
+    if (!across) {
+        rows(1, 1);
+        rows(1, 2);
+        rows(2, 1);
+        if (planes < 3) rows(2, 2);
+        if (planes == 1) {
+            rows(1, 4);
+            rows(4, 2);
+        }
     }
     if (planes < 3) {
         // 128 x 128: two workgroups on a compute unit, or one; packed codes have the same stages either way
@@ -111,13 +102,45 @@ hipError_t launch_linear(const LinearArgs &A0, int xbits, int wbits, int planes,
         tiles(kTileLarge, tile_us(A, wbits, 3, 384, 128, kCUs, 4.7, 1.24));
         tiles(kTileDeep, tile_us(A, wbits, 3, 192, 128, kCUs, 5.8, 0.71));
     }
-    if (few) {
-        if (xbits == 4) return launch_linear_rows4(A, wbits, blocks, cols, stream);
-        return launch_linear_rows8(A, wbits, planes, blocks, cols, stream);
+    return c;
+}
+
+bool quads(const LinearArgs &A) { return (uintptr_t)A.y % 16 == 0 && A.ldy * (A.dtype == BQ_F32 ? 4 : 2) % 16 == 0; }
+
+}  // namespace
+
+hipError_t launch_linear(const LinearArgs &A0, int xbits, int wbits, int planes, hipStream_t stream)
+{
+    LinearArgs A = A0;
+    A.factor /= (float)((1 << (8 - xbits)) * (1 << (8 - wbits)));
+    A.y_quads = quads(A);
+    if (!fast_layout(A, xbits, wbits)) return launch_linear_any(A, xbits, wbits, stream);
+    const Choice c = choose(A, xbits, wbits, planes, false);
+    if (c.few) {
+        if (xbits == 4) return launch_linear_rows4(A, wbits, c.blocks, c.cols, stream);
+        return launch_linear_rows8(A, wbits, planes, c.blocks, c.cols, stream);
     }
-    if (planes > 1) return launch_linear_tile_digits(A, planes, tile, stream);
-    if (xbits == 8) return launch_linear_tile8(A, wbits, tile, stream);
-    return launch_linear_tile4(A, wbits, tile, stream);
+    if (planes > 1) return launch_linear_tile_digits(A, planes, c.tile, stream);
+    if (xbits == 8) return launch_linear_tile8(A, wbits, c.tile, stream);
+    return launch_linear_tile4(A, wbits, c.tile, stream);
+}
+
+// Weights across save the transposition, its bytes at what the launch reaches that writes digits and transposes; the product's reads, 8
+// bytes instead of 16, make it 2 .. 4 % slower.  2048 rows of 4096 -> 4096, bf16: 8.2 + 59.2 us, transposed 13.5 + 57.7 us.
+bool linear_across_is_quicker(const LinearArgs &across, const LinearArgs &turned, int wbits, int planes)
+{
+    if (wbits < 4 || (uintptr_t)across.w % 16 != 0 || across.ldw % 16 != 0 || across.n * (int64_t)wbits % 128 != 0 || across.ldw >= (int64_t)1 << 23) return false;
+    const double used = !across.offsets ? 1.0 : across.experts < across.rows ? across.experts : (double)across.rows;
+    const double transposition = used * across.n * (across.k + across.w_rows * wbits / 8.0) / 5.0e6;
+    return 1.03 * choose(across, 8, wbits, planes, true).us < choose(turned, 8, 8, planes, false).us + transposition;
+}
+
+hipError_t launch_linear_across(const LinearArgs &A0, int wbits, int planes, hipStream_t stream)
+{
+    LinearArgs A = A0;
+    A.factor /= (float)(1 << (8 - wbits));
+    A.y_quads = quads(A);
+    return launch_linear_tile_across(A, wbits, planes, choose(A, 8, wbits, planes, true).tile, stream);
 }
 
 }  // namespace bq

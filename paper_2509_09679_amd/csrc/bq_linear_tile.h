@@ -46,19 +46,33 @@ __device__ __forceinline__ int w_turn(int row)
     return kRowBytes == 128 ? ((row >> 1) & 1) | ((row >> 3) & 4) : kRowBytes == 64 ? (row >> 4) & 2 : (row >> 4) & 1;
 }
 
-template <int kXBits, int kWBits, int kPlanes, typename Shape>
+// f for weights that lie across, rows of kRowBytes: a transposing read takes 8 bytes per lane, 32 lanes at a time, of 16 neighbouring
+// bytes of 8 rows (8 bits) or 8 of 16 rows (4 bits) from either of two places 32 rows apart.  (Two lanes per bank with 4 bits in rows
+// of 128 bytes; they move half as much.)
+template <int kRowBytes, int kBits>
+__device__ __forceinline__ int across_turn(int row)
+{
+    if (kBits == 8) return kRowBytes == 256 ? (row & 7) | ((row >> 2) & 8) : ((row >> 1) & 3) | ((row >> 3) & 4);
+    return kRowBytes == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+}
+
+// kAcross: the weights lie with the channels contiguous, [summed index][channel], and a stage is 128 rows of them; what a lane needs, 16
+// codes of one channel, comes out of LDS by reads that transpose.  Piece j of the first operand is then channels 16 j .. 16 j + 15.
+template <int kXBits, int kWBits, int kPlanes, typename Shape, bool kAcross = false>
 __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearArgs A)
 {
     typedef TileStages<kXBits, kWBits, Shape> Stages;
     constexpr int kSteps = Stages::steps, kDepth = Stages::depth;
     constexpr int kXRow = Stages::x_row, kWRow = Stages::w_row;
     constexpr int kXWords = kXRow / 16, kWWords = kWRow / 16;  // of a lane: 32 codes of every 16-row piece
+    constexpr int kWLine = kAcross ? Shape::w_rows * kWBits / 8 : kWRow;  // bytes of w's rows in LDS
+    static_assert(!kAcross || (kXBits == 8 && kWBits >= 4), "digits, and codes that the transposing reads know");
     constexpr int kXBytes = Shape::x_rows * kXRow, kWBytes = Shape::w_rows * kWRow, kStage = kXBytes + kWBytes;
     constexpr int kXLoads = kXBytes / 1024 / Shape::waves, kWLoads = kWBytes / 1024 / Shape::waves;
     static_assert(kXLoads * 1024 * Shape::waves == kXBytes && kWLoads * 1024 * Shape::waves == kWBytes, "whole loads per wave");
     static_assert(Shape::pieces % kPlanes == 0 && (kPlanes == 1 || kXBits == 8), "planes of a token in one wave");
     constexpr int kTokens = Shape::x_rows / kPlanes, kP = Shape::pieces;
-    constexpr bool kNatural = kXBits != kWBits;
+    constexpr bool kNatural = kXBits != kWBits && !kAcross;  // (digits are written in the order that they meet)
     extern __shared__ __align__(16) uint8_t tile_lds[];
 
     // which tile: workgroups go round the 8 XCDs, each of which takes a contiguous eighth of the tiles; within it 8 tiles along the
@@ -95,13 +109,19 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
         x_base[i] = A.x + plane * A.plane_step + rt.row0 * A.ldx;
         x_off[i] = (uint32_t)(token < last ? token : last) * (uint32_t)A.ldx + x_piece[i] * 16;
     }
-    w_base = A.w + rt.expert * A.w_step + (int64_t)o0 * A.ldw;
+    w_base = A.w + rt.expert * A.w_step + (kAcross ? (int64_t)o0 * kWBits / 8 : (int64_t)o0 * A.ldw);
 #pragma unroll
     for (int i = 0; i < kWLoads; ++i) {
-        const int row = (i * Shape::waves + wave) * (1024 / kWRow) + lane / (kWRow / 16);
-        const int last = A.n - o0 - 1;
-        w_piece[i] = (lane % (kWRow / 16)) ^ w_turn<kWRow>(row);
-        w_off[i] = (uint32_t)(row < last ? row : last) * (uint32_t)A.ldw + w_piece[i] * 16;
+        const int row = (i * Shape::waves + wave) * (1024 / kWLine) + lane / (kWLine / 16);
+        if constexpr (kAcross) {
+            const int piece = (lane % (kWLine / 16)) ^ across_turn<kWLine, kWBits>(row), last = (int)((int64_t)(A.n - o0) * kWBits / 128) - 1;
+            w_piece[i] = row;
+            w_off[i] = (uint32_t)row * (uint32_t)A.ldw + (piece < last ? piece : last) * 16;
+        } else {
+            const int last = A.n - o0 - 1;
+            w_piece[i] = (lane % (kWRow / 16)) ^ w_turn<kWRow>(row);
+            w_off[i] = (uint32_t)(row < last ? row : last) * (uint32_t)A.ldw + w_piece[i] * 16;
+        }
     }
     const int stages = (A.k + 64 * kSteps - 1) / (64 * kSteps);
     const int x_tail = (int)((int64_t)A.k * kXBits / 128) % (kXRow / 16), w_tail = (int)((int64_t)A.k * kWBits / 128) % (kWRow / 16);  // pieces of the last stage
@@ -111,6 +131,10 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
         if (n < kXLoads) {
             const bool missing = x_tail && s == stages - 1 && x_piece[n] >= x_tail;  // a piece behind the last input: any other one
             load_to_lds(at + n * Shape::waves * 1024, missing ? x_off[n] - x_piece[n] * 16 : x_off[n], x_base[n] + (int64_t)s * kXRow);
+        } else if constexpr (kAcross) {
+            // rows behind the last: the last one (the digits there are 0)
+            const int i = n - kXLoads, behind = s == stages - 1 ? s * 128 + w_piece[i] - (A.w_rows - 1) : 0;
+            load_to_lds(at + kXBytes + i * Shape::waves * 1024, w_off[i] - (behind > 0 ? behind * (uint32_t)A.ldw : 0u), w_base + (int64_t)s * 128 * A.ldw);
         } else {
             const int i = n - kXLoads;
             const bool missing = w_tail && s == stages - 1 && w_piece[i] >= w_tail;
@@ -126,7 +150,23 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
                                          (((kXWords == 8 ? 2 * g : g) + h) ^ lds_turn<kXRow, kXWords / 4>(r16)) * 16);
         v[4 * h] = q.x; v[4 * h + 1] = q.y; v[4 * h + 2] = q.z; v[4 * h + 3] = q.w;
     };
-    auto read_w = [&](int place, int j, int h, uint32_t (&v)[4][kWWords]) {
+    // (across: the address that a lane gives is another one's row)
+    const int across_row = 32 * g + (kWBits == 8 ? r16 >> 1 : r16);
+    const int across_at = across_row * kWLine + ((wave_n * (kWBits / 2)) ^ across_turn<kWLine, kWBits>(across_row)) * 16 + (kWBits == 8 ? r16 & 1 : 0) * 8;
+    auto read_w = [&](int place, int n, int h, uint32_t (&v)[4][kWWords]) {
+        const int j = n % 4;
+        if constexpr (kAcross) {
+            const int rows = h * 16 + n / 4 * 8, word = (kWBits == 8 ? 4 : 2) * h + n / 4 * 2;
+            const int at = place * kStage + kXBytes + (kWBits == 8 ? across_at ^ (j * 16) : (across_at ^ (j / 2 * 16)) + j % 2 * 8) + rows * kWLine;
+            typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+            i32x2 q;
+            if constexpr (kWBits == 8)
+                q = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(tile_lds + at));
+            else
+                q = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)(tile_lds + at));
+            v[j][word] = (uint32_t)q[0]; v[j][word + 1] = (uint32_t)q[1];
+            return;
+        }
         const uint8_t *p = tile_lds + place * kStage + kXBytes + (w_row + j * 4) * kWRow;
         if constexpr (kWBits == 2) {
             const uint2 q = *(const uint2 *)(p + ((g >> 1) ^ w_turn<kWRow>(w_row)) * 16 + (g & 1) * 8);
@@ -152,18 +192,19 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
     // the barrier the reads of 8 waves would hold up everyone's products.
     constexpr int kRing = kP % 4 == 0 ? 4 : 3;
     static_assert(kP % kRing == 0 && kP >= 4, "the ring's places are the same in every stage");
-    constexpr int kXReads = kXWords / 4, kWReads = kWWords == 8 ? 8 : 4;  // of a piece of x; of all of w
+    constexpr int kWTurns = kAcross || kWWords == 8 ? 2 : 1, kWEach = kAcross && kWBits == 8 ? 8 : 4;
+    constexpr int kXReads = kXWords / 4, kWReads = kWTurns * kWEach;  // of a piece of x; of all of w
     constexpr int kFirst = kWReads + 2 * kXReads;  // reads that a stage starts from
     i32x4 acc[kP][4] = {};
     uint32_t wv[2][4][kWWords], xv[kRing][kXWords];  // (w's codes alternate: in one array every stage began by copying them)
     auto first_read = [&](int place, int n, uint32_t (&wv)[4][kWWords]) {
         // w's first halves, x's first piece, w's other halves, x's second piece
-        if (n < 4)
+        if (n < kWEach)
             read_w(place, n, 0, wv);
-        else if (n < 4 + kXReads)
-            read_x(place, 0, n - 4, xv[0]);
+        else if (n < kWEach + kXReads)
+            read_x(place, 0, n - kWEach, xv[0]);
         else if (n < kWReads + kXReads)
-            read_w(place, n - 4 - kXReads, 1, wv);
+            read_w(place, n - kWEach - kXReads, 1, wv);
         else
             read_x(place, 1, n - kWReads - kXReads, xv[1]);
     };
@@ -244,6 +285,29 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
     }
     stage(s, place, 0, wv[0], wv[1], std::integral_constant<int, 0>{});
 
+    if constexpr (kAcross) {  // a gradient has no scales and no bias of the channels
+        const int o = o0 + wave_n * 64 + g * 4;
+#pragma unroll
+        for (int i = 0; i < kP / kPlanes; ++i) {
+            const int64_t t = rt.row0 + (wave_t * (kP / kPlanes) + i) * 16 + r16;
+            if (t >= rt.row_end) continue;
+            const float s = load_scale(A.xs, t, A.xs_f16) * A.factor;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (o + 16 * j >= A.n) continue;
+                float v[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    int part[kPlanes];
+#pragma unroll
+                    for (int p = 0; p < kPlanes; ++p) part[p] = acc[i * kPlanes + p][j][r];
+                    v[r] = joined<kPlanes>(part) * s;
+                }
+                store_results<4>(A, t * A.ldy + o + 16 * j, v, A.n - o - 16 * j, A.y_quads);
+            }
+        }
+        return;
+    }
     const int o = o0 + wave_n * 64 + g * 16;
     if (o >= A.n) return;
     float ws[16], bias[16];
@@ -278,16 +342,16 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
     }
 }
 
-template <int kXBits, int kWBits, int kPlanes, typename Shape>
+template <int kXBits, int kWBits, int kPlanes, typename Shape, bool kAcross = false>
 hipError_t launch_tile(const LinearArgs &A, hipStream_t stream)
 {
     constexpr size_t kLds = (size_t)TileStages<kXBits, kWBits, Shape>::depth * TileStages<kXBits, kWBits, Shape>::bytes;
     static LdsLimitOnce limit;
-    const hipError_t e = limit.set((const void *)linear_tile_kernel<kXBits, kWBits, kPlanes, Shape>, kLds);
+    const hipError_t e = limit.set((const void *)linear_tile_kernel<kXBits, kWBits, kPlanes, Shape, kAcross>, kLds);
     if (e != hipSuccess) return e;
     const int64_t n_tiles = (A.n + Shape::w_rows - 1) / Shape::w_rows;
     const int64_t all = row_tiles_bound(A, Shape::x_rows / kPlanes) * n_tiles;
-    hipLaunchKernelGGL((linear_tile_kernel<kXBits, kWBits, kPlanes, Shape>), dim3((unsigned)((all + 7) / 8 * 8)), dim3(Shape::threads), kLds,
+    hipLaunchKernelGGL((linear_tile_kernel<kXBits, kWBits, kPlanes, Shape, kAcross>), dim3((unsigned)((all + 7) / 8 * 8)), dim3(Shape::threads), kLds,
                        stream, A);
     return hipGetLastError();
 }

@@ -423,7 +423,7 @@ BATCHES_FWD = [(1, 18, 64, 0), (3, 1500, 64, 3), (115, 520, 64, 0), (200, 650, 6
                (115, 2050, 64, 0), (450, 2050, 64, 0), (187, 520, 64, 3), (115, 1500, 64, 3), (115, 4100, 64, 0), (380, 330, 64, 0), (390, 4100, 832, 0),
                (200, 20000, 64, 3), (300, 20000, 64, 3), (4100, 2050, 64, 50), (4096, 16, 64, 64)]
 BATCHES_BWD = [(1, 18, 0), (150, 200, 3), (200, 330, 0), (200, 300, 3), (700, 200, 0), (600, 200, 0), (830, 780, 0), (450, 520, 0), (390, 650, 0),
-               (420, 1500, 0), (4100, 520, 50), (600, 6000, 3), (4100, 780, 50), (4096, 16, 64)]
+               (420, 1500, 0), (4100, 520, 50), (600, 6000, 3), (600, 6008, 3), (4100, 780, 50), (4096, 16, 64)]
 
 
 @pytest.mark.parametrize("xbits,wbits", BITS)
@@ -447,13 +447,15 @@ def test_batches_fwd(T, N, K, experts, xbits, wbits):
     assert (y[:offsets[0]] == 3).all() and (y[offsets[-1]:] == 3).all()
 
 
-def _check_bwd(T, N, K, experts, wbits, dtype, scale, seed):
+def _check_bwd(T, N, K, experts, wbits, dtype, scale, seed, pad_w=0, pad_dx=0):
     gen = torch.Generator(device=DEV).manual_seed(seed)
     E, offsets = max(1, experts), _ragged(T, experts) if experts else [0, T]
     qw, w = _codes_on_device(gen, (E, N, K), wbits)
     ws = (torch.rand((E, N), generator=gen, device=DEV) * 0.01 + 1e-3).to(TORCH[scale])
     dy = (torch.randn((T, N), generator=gen, device=DEV) * torch.exp(torch.randn((T, 1), generator=gen, device=DEV))).to(TORCH[dtype])
-    dx = torch.full((T, K), 3.0, dtype=TORCH[dtype], device=DEV)
+    w = torch.cat([w, torch.full((E, N, pad_w), 7, dtype=torch.int8, device=DEV)], 2)[..., :w.shape[2]]
+    padded = torch.full((T, K + pad_dx), 3.0, dtype=TORCH[dtype], device=DEV)
+    dx = padded[:, :K]
     wd, wsd = (w, ws) if experts else (w[0], ws[0])
     d = B.make_linear_bwd(dy, wd, wsd, dx, wbits=wbits)
     work = torch.full((B.bq_linear_bwd_workspace_bytes(d),), 0xA5, dtype=torch.uint8, device=DEV)
@@ -470,7 +472,19 @@ def _check_bwd(T, N, K, experts, wbits, dtype, scale, seed):
         want = v @ qw[e]
         f32 = term * v.abs().amax(1, keepdim=True) * qw[e].abs().sum(0) + 2 * 2.0 ** -24 * want.abs()
         _within(dx[lo:hi], want, f32 + (lu.half_step(dtype) * (want.abs() + f32) + lu.smallest(dtype) if dtype != "f32" else 0) + 1e-40)
-    assert (dx[:offsets[0]] == 3).all() and (dx[offsets[-1]:] == 3).all()
+    assert (dx[:offsets[0]] == 3).all() and (dx[offsets[-1]:] == 3).all() and (padded[:, K:] == 3).all()
+
+
+# as many rows as make it worth while to read the weights as they lie: the sum's length and the inputs around tiles' ends, the smallest sums
+ACROSS = [(19, 10, 20000, 0, 0), (300, 520, 2080, 0, 16), (115, 10, 20000, 3, 0), (150, 10, 20000, 3, 32), (4100, 10, 544, 50, 0), (700, 1100, 1568, 0, 48),
+          (1000, 130, 672, 3, 0), (255, 777, 992, 0, 0), (2040, 384, 256, 0, 16), (3000, 1, 288, 0, 0), (999, 128, 2336, 3, 0), (513, 129, 1056, 0, 0)]
+
+
+@pytest.mark.parametrize("wbits", [8, 4])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,N,K,experts,pad_w", ACROSS)
+def test_bwd_on_weights_as_they_lie(T, N, K, experts, pad_w, dtype, wbits):
+    _check_bwd(T, N, K, experts, wbits, dtype, "f32", T + N + K, pad_w=pad_w, pad_dx=5 if T % 2 else 8)
 
 
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
@@ -488,9 +502,18 @@ def test_bwd_of_wide_layers(N, dtype, wbits):
     _check_bwd(37, N, 80, 4, wbits, dtype, "f32" if N % 3 else "f16", N + 1)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("N", [512, 1032, 2504, 8000, 16376])
+def test_bwd_of_wide_layers_on_weights_as_they_lie(N, dtype):
+    _check_bwd(700, N, 1056, 0, 8, dtype, "f16", N)
+    _check_bwd(390, N, 1056, 3, 4, dtype, "f32", N + 1)
+
+
 def test_bwd_of_more_rows_than_workgroups():
     _check_bwd(4096 * 2 + 77, 256, 64, 0, 8, "bf16", "f32", 1)
     _check_bwd(4096 * 2 + 77, 250, 64, 3, 4, "f16", "f32", 2)
+    _check_bwd(16384 * 2 + 77, 256, 128, 0, 8, "bf16", "f32", 3)
+    _check_bwd(16384 * 2 + 77, 1024, 128, 3, 4, "f32", "f32", 4)
 
 
 # ---- places beyond 2^32 ---------------------------------------------------------------------------------

@@ -30,7 +30,6 @@ struct LinearArgs {
     int k, n, experts;
     int xs_f16, ws_f16, dtype;
     float factor;  // of the fields' positions
-    int y_quads;   // rows of y are 16-byte aligned
     int w_rows;    // of weights that lie across (bq_linear_tile.h): the summed index may be padded beyond it
 };
 

@@ -105,15 +105,12 @@ Choice choose(const LinearArgs &A, int xbits, int wbits, int planes, bool across
     return c;
 }
 
-bool quads(const LinearArgs &A) { return (uintptr_t)A.y % 16 == 0 && A.ldy * (A.dtype == BQ_F32 ? 4 : 2) % 16 == 0; }
-
 }  // namespace
 
 hipError_t launch_linear(const LinearArgs &A0, int xbits, int wbits, int planes, hipStream_t stream)
 {
     LinearArgs A = A0;
     A.factor /= (float)((1 << (8 - xbits)) * (1 << (8 - wbits)));
-    A.y_quads = quads(A);
     if (!fast_layout(A, xbits, wbits)) return launch_linear_any(A, xbits, wbits, stream);
     const Choice c = choose(A, xbits, wbits, planes, false);
     if (c.few) {
@@ -139,7 +136,6 @@ hipError_t launch_linear_across(const LinearArgs &A0, int wbits, int planes, hip
 {
     LinearArgs A = A0;
     A.factor /= (float)(1 << (8 - wbits));
-    A.y_quads = quads(A);
     return launch_linear_tile_across(A, wbits, planes, choose(A, 8, wbits, planes, true).tile, stream);
 }
 

@@ -8,8 +8,8 @@
 // with an infinity or NaN gets f = NaN: its gradient is NaN throughout.
 #include <type_traits>
 
-#include "bq_cascade.h"
 #include "bq_linear_codes.h"
+#include "bq_piece.h"
 
 namespace bq {
 
@@ -112,11 +112,11 @@ __device__ __forceinline__ void digits8(float (&v)[8], const RowFactor &f, int o
                         : make_uint2(w[p][0], w[p][1]);
 }
 
-// Rows of whole, aligned pieces of 8.  kThreads, a wave or the workgroup, take rows_each neighbouring rows, which mostly belong to one
-// expert, and keep that expert's scales and a row's products in registers; kPasses pieces per thread.  One read of dy and one write of
+// kThreads, a wave or the workgroup, take rows_each neighbouring rows, which mostly belong to one
+// expert, and keep that expert's scales and a row's products in registers; kPasses pieces per thread.  kWhole: the rows' pieces are whole.  One read of dy and one write of
 // the digits: bound by HBM, and for a few thousand rows by the one turn to memory that a row's largest entry takes.  4096 rows of 1408 of 8
 // experts: 8.8 us with workgroups, 7.9 us with waves.
-template <typename T, int kPlanes, int kThreads, int kPasses>
+template <typename T, int kPlanes, int kThreads, int kPasses, bool kWhole>
 __device__ __forceinline__ void digit_rows(const DigitArgs &A, int64_t block, int rows_each)
 {
     const int thread = threadIdx.x % kThreads;
@@ -126,11 +126,11 @@ __device__ __forceinline__ void digit_rows(const DigitArgs &A, int64_t block, in
     int expert = -1;
     for (int64_t row = first; row < end; ++row) {
         const T *dy = (const T *)A.dy + row * A.ld_dy;
-        Raw8 raw[kPasses];
+        Raw8 raw[kPasses];  // (asked for ahead of the expert, whose place takes two more turns to memory)
 #pragma unroll
-        for (int p = 0; p < kPasses; ++p) {  // (asked for ahead of the expert, whose place takes two more turns to memory)
-            const int c = (p * kThreads + thread) * 8;
-            raw[p] = load8(dy + (c < A.n ? c : 0));
+        for (int p = 0; p < kPasses; ++p) {
+            const int c = (p * kThreads + thread) * 8, at = c < A.n ? c : 0;
+            raw[p] = kWhole ? load_whole_piece(dy + at) : load_piece(dy + at, A.n - c);
         }
         const int e = expert_of(A.offsets, A.experts, row);
         if (e < 0) continue;  // (the product does not look at it)
@@ -140,10 +140,11 @@ __device__ __forceinline__ void digit_rows(const DigitArgs &A, int64_t block, in
             for (int p = 0; p < kPasses; ++p) {
                 const int c = (p * kThreads + thread) * 8;
                 const int64_t at = (int64_t)e * A.n + (c < A.n ? c : 0);
+                const int left = kWhole ? 8 : A.n - c;
                 if (A.ws_f16)
-                    unpack8(load8((const __half *)A.ws + at), ws[p], (const __half *)nullptr);
+                    unpack8(load_piece((const __half *)A.ws + at, left), ws[p], (const __half *)nullptr);
                 else
-                    unpack8(load8((const float *)A.ws + at), ws[p], (const float *)nullptr);
+                    unpack8(load_piece((const float *)A.ws + at, left), ws[p], (const float *)nullptr);
             }
         }
         float v[kPasses][8];
@@ -173,9 +174,9 @@ __device__ __forceinline__ void digit_rows(const DigitArgs &A, int64_t block, in
     }
 }
 
-// Any rows; the second look at a row comes from the caches.
+// Wider rows; the second look at a row comes from the caches.
 template <typename T, int kPlanes>
-__device__ __forceinline__ void digit_rows_any(const DigitArgs &A, int64_t block, int rows_each)
+__device__ __forceinline__ void digit_rows_wide(const DigitArgs &A, int64_t block, int rows_each)
 {
     const int64_t end = (block + 1) * rows_each < A.rows ? (block + 1) * rows_each : A.rows;
     for (int64_t row = block * rows_each; row < end; ++row) {
@@ -266,9 +267,9 @@ __device__ __forceinline__ void transpose_tile(const TransposeArgs &A, uint32_t 
     }
 }
 
-// Both in one launch: neither needs the other.  The first digit_blocks workgroups write digits (kPasses 0: of any rows), the others
+// Both in one launch: neither needs the other.  The first digit_blocks workgroups write digits (kPasses 0: of the widest rows), the others
 // transpose (kBits 0: there are none).
-template <typename T, int kPlanes, int kThreads, int kPasses, int kBits>
+template <typename T, int kPlanes, int kThreads, int kPasses, bool kWhole, int kBits>
 __global__ __launch_bounds__(256) void linear_prepare_kernel(DigitArgs D, int rows_each, uint32_t digit_blocks, TransposeArgs R)
 {
     if constexpr (kBits != 0) {
@@ -278,9 +279,9 @@ __global__ __launch_bounds__(256) void linear_prepare_kernel(DigitArgs D, int ro
         }
     }
     if constexpr (kPasses == 0)
-        digit_rows_any<T, kPlanes>(D, blockIdx.x, rows_each);
+        digit_rows_wide<T, kPlanes>(D, blockIdx.x, rows_each);
     else
-        digit_rows<T, kPlanes, kThreads, kPasses>(D, blockIdx.x, rows_each);
+        digit_rows<T, kPlanes, kThreads, kPasses, kWhole>(D, blockIdx.x, rows_each);
 }
 
 // The same for any width and alignment, 64 x 64 codes one by one.
@@ -309,20 +310,22 @@ int padded(int n) { return (n + 127) / 128 * 128; }
 template <typename T, int kPlanes, int kBits>
 hipError_t launch_prepare(const DigitArgs &D, const TransposeArgs &R, uint32_t transpose_blocks, hipStream_t stream)
 {
-    const bool whole = (uintptr_t)D.dy % 16 == 0 && D.ld_dy * sizeof(T) % 16 == 0 && D.n % 8 == 0 && (uintptr_t)D.ws % 16 == 0 && D.np <= 16384;
     auto launch = [&](auto THREADS, auto PASSES) {
         constexpr int threads = decltype(THREADS)::value, passes = decltype(PASSES)::value, at_once = 256 / threads;
         // beyond 16384 waves they take several rows each
         const int rows_each = (int)((D.rows + 4096 * at_once - 1) / (4096 * at_once));
         const int64_t per_block = (int64_t)rows_each * at_once;
         const uint32_t digit_blocks = (uint32_t)((D.rows + per_block - 1) / per_block);
-        hipLaunchKernelGGL((linear_prepare_kernel<T, kPlanes, threads, passes, kBits>), dim3(digit_blocks + transpose_blocks), dim3(256), 0, stream, D,
-                           rows_each, digit_blocks, R);
+        const dim3 grid(digit_blocks + transpose_blocks);
+        if (passes == 0 || D.n % 8 == 0)
+            hipLaunchKernelGGL((linear_prepare_kernel<T, kPlanes, threads, passes, true, kBits>), grid, dim3(256), 0, stream, D, rows_each, digit_blocks, R);
+        else
+            hipLaunchKernelGGL((linear_prepare_kernel<T, kPlanes, threads, passes, passes == 0, kBits>), grid, dim3(256), 0, stream, D, rows_each, digit_blocks, R);
         return hipGetLastError();
     };
     typedef std::integral_constant<int, 64> Wave;
     typedef std::integral_constant<int, 256> Workgroup;
-    if (!whole) return launch(Workgroup{}, std::integral_constant<int, 0>{});
+    if (D.np > 16384) return launch(Workgroup{}, std::integral_constant<int, 0>{});
     if constexpr (kBits == 0) {
         // (beside transposing workgroups their registers cost more than the barrier of a workgroup's row)
         if (D.np <= 512) return launch(Wave{}, std::integral_constant<int, 1>{});

@@ -129,14 +129,14 @@ __device__ __forceinline__ void channel_bias(const LinearArgs &A, const int64_t 
     }
 }
 
-// kCount (a multiple of 4) consecutive results of one row, `left` of them inside the row; vec: 4 results at a time are aligned
+// kCount (a multiple of 4) consecutive results of one row at any address, `left` of them inside the row
 template <int kCount>
-__device__ __forceinline__ void store_results(const LinearArgs &A, int64_t at, const float (&v)[kCount], int left, bool vec)
+__device__ __forceinline__ void store_results(const LinearArgs &A, int64_t at, const float (&v)[kCount], int left)
 {
-    if (vec && left >= kCount) {
+    if (left >= kCount) {
         if (A.dtype == BQ_F32) {
 #pragma unroll
-            for (int j = 0; j < kCount; j += 4) *(float4 *)((float *)A.y + at + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            for (int j = 0; j < kCount; j += 4) __builtin_memcpy((float *)A.y + at + j, v + j, 16);
             return;
         }
         uint32_t w[kCount / 2];
@@ -146,10 +146,10 @@ __device__ __forceinline__ void store_results(const LinearArgs &A, int64_t at, c
         uint16_t *p = (uint16_t *)A.y + at;
         if constexpr (kCount % 8 == 0) {
 #pragma unroll
-            for (int j = 0; j < kCount / 2; j += 4) *(uint4 *)(p + 2 * j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+            for (int j = 0; j < kCount / 2; j += 4) __builtin_memcpy(p + 2 * j, w + j, 16);
         } else {
 #pragma unroll
-            for (int j = 0; j < kCount / 2; j += 2) *(uint2 *)(p + 2 * j) = make_uint2(w[j], w[j + 1]);
+            for (int j = 0; j < kCount / 2; j += 2) __builtin_memcpy(p + 2 * j, w + j, 8);
         }
         return;
     }

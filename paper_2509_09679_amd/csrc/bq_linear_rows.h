@@ -177,7 +177,7 @@ __global__ __launch_bounds__((64 * RowsShape<kXBits, kWBits, kPlanes, kBlocks, k
                 if (A.ws) v[r] *= ws[r];
                 if (A.bias) v[r] += bias[r];
             }
-            store_results<4>(A, t * A.ldy + o, v, A.n - o, A.y_quads);
+            store_results<4>(A, t * A.ldy + o, v, A.n - o);
         }
     }
 }

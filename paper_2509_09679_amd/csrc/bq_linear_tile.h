@@ -303,7 +303,7 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
                     for (int p = 0; p < kPlanes; ++p) part[p] = acc[i * kPlanes + p][j][r];
                     v[r] = joined<kPlanes>(part) * s;
                 }
-                store_results<4>(A, t * A.ldy + o + 16 * j, v, A.n - o - 16 * j, A.y_quads);
+                store_results<4>(A, t * A.ldy + o + 16 * j, v, A.n - o - 16 * j);
             }
         }
         return;
@@ -338,7 +338,7 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
             if (A.ws) v[c] *= ws[c];
             if (A.bias) v[c] += bias[c];
         }
-        store_results<16>(A, (t0 + 16 * i) * A.ldy + o, v, A.n - o, A.y_quads);
+        store_results<16>(A, (t0 + 16 * i) * A.ldy + o, v, A.n - o);
     }
 }
 

@@ -1,11 +1,16 @@
 // INT8 codes and one scale per row:  s = max |x| / 127,  q = clip(rint(x / s)).  One read of the rows, one write of the codes:
 // bound by HBM.  A row's entries stay in registers between the maximum and the codes.
-#include "bq_cascade.h"
+#include <type_traits>
+
 #include "bq_linear.h"
+#include "bq_piece.h"
 
 namespace bq {
 
 namespace {
+
+template <int kN>
+using N = std::integral_constant<int, kN>;
 
 struct RowQuantArgs {
     const void *x;
@@ -37,18 +42,20 @@ __device__ __forceinline__ int code8(float v, float inv)
     return inv == 0.0f ? 0 : (int)fminf(fmaxf(q, -128.0f), 127.0f);
 }
 
-__device__ __forceinline__ uint32_t wave_max(uint32_t m)
+template <int kLanes>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t m)
 {
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
+    for (int d = 1; d < (kLanes < 64 ? kLanes : 64); d <<= 1) {
         const uint32_t o = (uint32_t)__shfl_xor((int)m, d, 64);
         m = m > o ? m : o;
     }
     return m;
 }
 
-// kLanes threads per row (64: four rows per workgroup), kPasses pieces of 8 elements per thread.
-template <typename T, int kLanes, int kPasses>
+// kLanes threads per row (16 .. 64: several rows per workgroup), kPasses pieces of 8 elements per thread.  kWhole: a
+// row's pieces are whole (with a branch for the last one between the loads, 1777 rows of 5120 take 9.5 us instead of 8.6 us).
+template <typename T, int kLanes, int kPasses, bool kWhole>
 __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void row_quant_kernel(RowQuantArgs A)
 {
     constexpr int kThreads = kLanes < 256 ? 256 : kLanes, kRows = kThreads / kLanes;
@@ -64,14 +71,14 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void row_quant_kernel(
         const int c = (p * kLanes + lane) * 8;
 #pragma unroll
         for (int r = 0; r < 8; ++r) v[p][r] = 0.0f;
-        if (live && c < A.cols) unpack8(load8(x + c), v[p], (const T *)nullptr);
+        if (live && c < A.cols) unpack8(kWhole ? load_whole_piece(x + c) : load_piece(x + c, A.cols - c), v[p], (const T *)nullptr);
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
             const uint32_t b = __float_as_uint(v[p][r]) & 0x7FFFFFFFu;
             m = m > b ? m : b;
         }
     }
-    m = wave_max(m);
+    m = lanes_max<kLanes>(m);
     if (kLanes > 64) {
         if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = m;
         __syncthreads();
@@ -97,13 +104,13 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void row_quant_kernel(
         for (int h = 0; h < 2; ++h)
             w[h] = ((uint32_t)code8(v[p][4 * h], inv) & 255u) | ((uint32_t)code8(v[p][4 * h + 1], inv) & 255u) << 8 |
                    ((uint32_t)code8(v[p][4 * h + 2], inv) & 255u) << 16 | (uint32_t)code8(v[p][4 * h + 3], inv) << 24;
-        *(uint2 *)(out + c) = make_uint2(w[0], w[1]);
+        store_piece(out + c, make_uint2(w[0], w[1]), kWhole ? 8 : A.cols - c);
     }
 }
 
-// Rows of any width, stride and alignment, one workgroup each; the second look at the row comes from the caches.
+// Wider rows, one workgroup each; the second look at the row comes from the caches.
 template <typename T>
-__global__ __launch_bounds__(256) void row_quant_any_kernel(RowQuantArgs A)
+__global__ __launch_bounds__(256) void row_quant_wide_kernel(RowQuantArgs A)
 {
     __shared__ uint32_t s_max[4];
     for (int64_t row = blockIdx.x; row < A.rows; row += gridDim.x) {
@@ -113,7 +120,7 @@ __global__ __launch_bounds__(256) void row_quant_any_kernel(RowQuantArgs A)
             const uint32_t b = __float_as_uint(to_float(x[c])) & 0x7FFFFFFFu;
             m = m > b ? m : b;
         }
-        m = wave_max(m);
+        m = lanes_max<64>(m);
         __syncthreads();
         if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = m;
         __syncthreads();
@@ -135,31 +142,31 @@ __global__ __launch_bounds__(256) void row_quant_any_kernel(RowQuantArgs A)
 template <typename T>
 hipError_t launch_typed(const RowQuantArgs &A, hipStream_t stream)
 {
-    const bool vec = (uintptr_t)A.x % 16 == 0 && (uintptr_t)A.codes % 8 == 0 && A.ld_x * sizeof(T) % 16 == 0 && A.ld_codes % 8 == 0 &&
-                     A.cols % 8 == 0 && A.cols <= 32768;
-    if (!vec) {
-        hipLaunchKernelGGL(row_quant_any_kernel<T>, dim3((unsigned)(A.rows < 65536 ? A.rows : 65536)), dim3(256), 0, stream, A);
+    if (A.cols > 32768) {
+        hipLaunchKernelGGL(row_quant_wide_kernel<T>, dim3((unsigned)(A.rows < 65536 ? A.rows : 65536)), dim3(256), 0, stream, A);
         return hipGetLastError();
     }
-    // (threads along a dimension of a launch are counted in 32 bits)
-    auto grid = [](int64_t groups) { return dim3((unsigned)(groups < 1 << 20 ? groups : 1 << 20), (unsigned)((groups + (1 << 20) - 1) >> 20)); };
-    const dim3 rows = grid(A.rows), quads = grid((A.rows + 3) / 4);
-    const int eights = A.cols / 8;
-    if (eights <= 64)
-        hipLaunchKernelGGL((row_quant_kernel<T, 64, 1>), quads, dim3(256), 0, stream, A);
-    else if (eights <= 128)
-        hipLaunchKernelGGL((row_quant_kernel<T, 64, 2>), quads, dim3(256), 0, stream, A);
-    else if (eights <= 256)
-        hipLaunchKernelGGL((row_quant_kernel<T, 256, 1>), rows, dim3(256), 0, stream, A);
-    else if (eights <= 512)
-        hipLaunchKernelGGL((row_quant_kernel<T, 256, 2>), rows, dim3(256), 0, stream, A);
-    else if (eights <= 1024)
-        hipLaunchKernelGGL((row_quant_kernel<T, 256, 4>), rows, dim3(256), 0, stream, A);
-    else if (eights <= 2048)
-        hipLaunchKernelGGL((row_quant_kernel<T, 512, 4>), rows, dim3(512), 0, stream, A);
-    else
-        hipLaunchKernelGGL((row_quant_kernel<T, 1024, 4>), rows, dim3(1024), 0, stream, A);
-    return hipGetLastError();
+    auto launch = [&](auto LANES, auto PASSES) {
+        constexpr int lanes = decltype(LANES)::value, passes = decltype(PASSES)::value, threads = lanes < 256 ? 256 : lanes;
+        // (threads along a dimension of a launch are counted in 32 bits)
+        const int64_t groups = (A.rows + threads / lanes - 1) / (threads / lanes);
+        const dim3 grid((unsigned)(groups < 1 << 20 ? groups : 1 << 20), (unsigned)((groups + (1 << 20) - 1) >> 20));
+        if (A.cols % 8 == 0)
+            hipLaunchKernelGGL((row_quant_kernel<T, lanes, passes, true>), grid, dim3(threads), 0, stream, A);
+        else
+            hipLaunchKernelGGL((row_quant_kernel<T, lanes, passes, false>), grid, dim3(threads), 0, stream, A);
+        return hipGetLastError();
+    };
+    const int eights = (A.cols + 7) / 8;
+    if (eights <= 16) return launch(N<16>{}, N<1>{});
+    if (eights <= 32) return launch(N<32>{}, N<1>{});
+    if (eights <= 64) return launch(N<64>{}, N<1>{});
+    if (eights <= 128) return launch(N<64>{}, N<2>{});
+    if (eights <= 256) return launch(N<256>{}, N<1>{});
+    if (eights <= 512) return launch(N<256>{}, N<2>{});
+    if (eights <= 1024) return launch(N<256>{}, N<4>{});
+    if (eights <= 2048) return launch(N<512>{}, N<4>{});
+    return launch(N<1024>{}, N<4>{});
 }
 
 }  // namespace

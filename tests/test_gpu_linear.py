@@ -29,7 +29,8 @@ def _quant8_reference(x, scale):
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (5, 8), (1, 4096), (37, 512), (9, 520), (6, 1024), (7, 1032), (4, 2048), (5, 2056), (2, 5120),
-                                       (3, 8200), (2, 16384), (2, 16392), (1, 32768), (2, 32776), (3, 11008), (1030, 40)])
+                                       (3, 8200), (2, 16384), (2, 16392), (1, 32768), (2, 32776), (3, 11008), (1030, 40), (67, 120), (35, 200),
+                                       (21, 225), (13, 505), (6, 1001), (5, 2047), (3, 4081), (3, 8189), (2, 16383), (2, 32767), (2, 32769)])
 def test_rows_quant8_is_bit_exact(dtype, rows, cols):
     rng = np.random.default_rng([rows, cols, len(dtype)])
     for scale, pad, shift in (("f32", 0, 0), ("f16", 8, 0), ("f32", 3, 1)):
@@ -46,7 +47,7 @@ def test_rows_quant8_is_bit_exact(dtype, rows, cols):
             assert (gap == 7).all()
 
 
-@pytest.mark.parametrize("cols", [5, 64, 1024, 5120, 40000])
+@pytest.mark.parametrize("cols", [5, 64, 131, 1024, 2047, 5120, 40000])
 def test_rows_quant8_special_rows(cols):
     x = torch.randn(7, cols, device=DEV)
     x[0] = 0
@@ -91,8 +92,8 @@ def test_linear_fwd(T, N, K, xbits, wbits):
         lu.check(lu.f64(L.forward()), want, lu.bound_fwd(want, size, dtype), f"{dtype}")
 
 
-@pytest.mark.parametrize("T,N,K", [(4, 40, 96), (70, 200, 512), (300, 264, 256)])
-@pytest.mark.parametrize("pads", [(16, 16, 8, 0), (1, 3, 1, 1), (0, 0, 5, 0), (32, 0, 0, 16), (0, 0, 0, 5)])
+@pytest.mark.parametrize("T,N,K", [(4, 40, 96), (70, 200, 512), (300, 264, 256), (600, 2051, 384)])
+@pytest.mark.parametrize("pads", [(16, 16, 8, 0), (16, 0, 1, 0), (1, 3, 1, 1), (0, 0, 5, 0), (32, 0, 0, 16), (0, 0, 0, 5)])
 def test_linear_fwd_strides_and_alignment(T, N, K, pads):
     rng = np.random.default_rng([T, N, K, *pads])
     for bits in ((8, 8), (4, 2)):
@@ -447,12 +448,15 @@ def test_batches_fwd(T, N, K, experts, xbits, wbits):
     assert (y[:offsets[0]] == 3).all() and (y[offsets[-1]:] == 3).all()
 
 
-def _check_bwd(T, N, K, experts, wbits, dtype, scale, seed, pad_w=0, pad_dx=0):
+def _check_bwd(T, N, K, experts, wbits, dtype, scale, seed, pad_w=0, pad_dx=0, shift=0):
     gen = torch.Generator(device=DEV).manual_seed(seed)
     E, offsets = max(1, experts), _ragged(T, experts) if experts else [0, T]
     qw, w = _codes_on_device(gen, (E, N, K), wbits)
     ws = (torch.rand((E, N), generator=gen, device=DEV) * 0.01 + 1e-3).to(TORCH[scale])
     dy = (torch.randn((T, N), generator=gen, device=DEV) * torch.exp(torch.randn((T, 1), generator=gen, device=DEV))).to(TORCH[dtype])
+    if shift:  # rows and scales that start at any element
+        dy = lu.strided(dy, 3, shift)
+        ws = lu.strided(ws.reshape(1, -1), 0, shift).view(E, N)
     w = torch.cat([w, torch.full((E, N, pad_w), 7, dtype=torch.int8, device=DEV)], 2)[..., :w.shape[2]]
     padded = torch.full((T, K + pad_dx), 3.0, dtype=TORCH[dtype], device=DEV)
     dx = padded[:, :K]
@@ -487,6 +491,13 @@ def test_bwd_on_weights_as_they_lie(T, N, K, experts, pad_w, dtype, wbits):
     _check_bwd(T, N, K, experts, wbits, dtype, "f32", T + N + K, pad_w=pad_w, pad_dx=5 if T % 2 else 8)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("T,N,K", [(33, 7, 40), (5, 500, 96), (70, 1003, 130), (300, 4096, 256), (9, 16384, 48), (12, 16390, 64)])
+def test_bwd_of_rows_that_start_anywhere(T, N, K, dtype):
+    for shift, experts in ((1, 0), (5, 3)):
+        _check_bwd(T, N, K, experts, 8, dtype, "f16" if shift == 1 else "f32", T + N, shift=shift)
+
+
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 @pytest.mark.parametrize("T,K,experts", BATCHES_BWD)
 def test_batches_bwd(T, K, experts, dtype):
@@ -495,7 +506,7 @@ def test_batches_bwd(T, K, experts, dtype):
 
 @pytest.mark.parametrize("wbits", [8, 4, 2])
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
-@pytest.mark.parametrize("N", [104, 2048, 2056, 4104, 8200, 16384, 16392, 1001])
+@pytest.mark.parametrize("N", [104, 2048, 2056, 4104, 8200, 16384, 16392, 1001, 2501, 7999, 16001, 16385])
 def test_bwd_of_wide_layers(N, dtype, wbits):
     # rows of digits from one piece of a workgroup to the widest that stay in registers, and those that do not
     _check_bwd(5, N, 48, 0, wbits, dtype, "f16" if N % 3 else "f32", N)
@@ -503,7 +514,7 @@ def test_bwd_of_wide_layers(N, dtype, wbits):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
-@pytest.mark.parametrize("N", [512, 1032, 2504, 8000, 16376])
+@pytest.mark.parametrize("N", [512, 1032, 2504, 8000, 16376, 505, 1411, 4095, 5063, 16383, 16400])
 def test_bwd_of_wide_layers_on_weights_as_they_lie(N, dtype):
     _check_bwd(700, N, 1056, 0, 8, dtype, "f16", N)
     _check_bwd(390, N, 1056, 3, 4, dtype, "f32", N + 1)

@@ -126,7 +126,7 @@ hipError_t launch_linear(const LinearArgs &A0, int xbits, int wbits, int planes,
 // bytes instead of 16, make it 2 .. 4 % slower.  2048 rows of 4096 -> 4096, bf16: 8.2 + 59.2 us, transposed 13.5 + 57.7 us.
 bool linear_across_is_quicker(const LinearArgs &across, const LinearArgs &turned, int wbits, int planes)
 {
-    if (wbits < 4 || (uintptr_t)across.w % 16 != 0 || across.ldw % 16 != 0 || across.n * (int64_t)wbits % 128 != 0 || across.ldw >= (int64_t)1 << 23) return false;
+    if ((uintptr_t)across.w % 16 != 0 || across.ldw % 16 != 0 || across.n * (int64_t)wbits % 128 != 0 || across.ldw >= (int64_t)1 << 23) return false;
     const double used = !across.offsets ? 1.0 : across.experts < across.rows ? across.experts : (double)across.rows;
     const double transposition = used * across.n * (across.k + across.w_rows * wbits / 8.0) / 5.0e6;
     return 1.03 * choose(across, 8, wbits, planes, true).us < choose(turned, 8, 8, planes, false).us + transposition;

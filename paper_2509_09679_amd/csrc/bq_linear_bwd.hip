@@ -22,7 +22,7 @@ struct DigitArgs {
     const int32_t *offsets;
     int64_t rows, ld_dy;
     int n, np, experts, ws_f16;
-    int odd_last;  // eight digits lie as 0, 2, 4, 6, 1, 3, 5, 7: how 4-bit codes come out of a word with the fewest steps
+    int odd_last;  // eight digits lie as 0, 2, 4, 6, 1, 3, 5, 7: how packed codes come out of a word with the fewest steps
 };
 
 // over a wave, or a workgroup of four
@@ -422,7 +422,7 @@ hipError_t launch_linear_bwd(const void *dy, int64_t ld_dy, const void *w, int w
     across.w_rows = n;
     const bool as_they_are = linear_across_is_quicker(across, A, wbits, planes);
     const int turn = as_they_are ? 0 : wbits;
-    D.odd_last = as_they_are && wbits == 4;
+    D.odd_last = as_they_are && wbits < 8;
     const hipError_t e = dtype == BQ_F32   ? prepare<float, 3>(D, R, turn, stream)
                          : dtype == BQ_F16 ? prepare<__half, 2>(D, R, turn, stream)
                                            : prepare<bf16_t, 2>(D, R, turn, stream);

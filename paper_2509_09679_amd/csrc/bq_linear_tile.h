@@ -47,17 +47,31 @@ __device__ __forceinline__ int w_turn(int row)
 }
 
 // f for weights that lie across, rows of kRowBytes: a transposing read takes 8 bytes per lane, 32 lanes at a time, of 16 neighbouring
-// bytes of 8 rows (8 bits) or 8 of 16 rows (4 bits) from either of two places 32 rows apart.  (Two lanes per bank with 4 bits in rows
-// of 128 bytes; they move half as much.)
+// bytes of 8 rows (8 bits) or 8 of 16 rows (4 and 2 bits) from either of two places 32 rows apart.  (The latter read every bank twice;
+// they move half as much.)
 template <int kRowBytes, int kBits>
 __device__ __forceinline__ int across_turn(int row)
 {
     if (kBits == 8) return kRowBytes == 256 ? (row & 7) | ((row >> 2) & 8) : ((row >> 1) & 3) | ((row >> 3) & 4);
-    return kRowBytes == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+    return kRowBytes == 128 ? (row >> 1) & 7 : kRowBytes == 64 ? (row >> 2) & 3 : (row >> 3) & 1;
+}
+
+// 16 codes of 2 bits out of two words of pairs, the even channel's (odd = 0) or the odd one's, as bytes that hold 64 times the code; 0, 2,
+// 4, 6, 1, 3, 5, 7 of either word
+__device__ __forceinline__ i32x4 pair_codes(const uint32_t (&w)[2], int odd)
+{
+    i32x4 r;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        r[2 * j] = (int)((odd ? w[j] << 4 : w[j] << 6) & 0xC0C0C0C0u);
+        r[2 * j + 1] = (int)((odd ? w[j] : w[j] << 2) & 0xC0C0C0C0u);
+    }
+    return r;
 }
 
 // kAcross: the weights lie with the channels contiguous, [summed index][channel], and a stage is 128 rows of them; what a lane needs, 16
-// codes of one channel, comes out of LDS by reads that transpose.  Piece j of the first operand is then channels 16 j .. 16 j + 15.
+// codes of one channel, comes out of LDS by reads that transpose.  Piece j of the first operand is then channels 16 j .. 16 j + 15; of
+// 2-bit codes, which are read as fields of 4 bits, the even or (odd j) the odd ones of 32 (j / 2) .. 32 (j / 2) + 31.
 template <int kXBits, int kWBits, int kPlanes, typename Shape, bool kAcross = false>
 __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearArgs A)
 {
@@ -66,10 +80,11 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
     constexpr int kXRow = Stages::x_row, kWRow = Stages::w_row;
     constexpr int kXWords = kXRow / 16, kWWords = kWRow / 16;  // of a lane: 32 codes of every 16-row piece
     constexpr int kWLine = kAcross ? Shape::w_rows * kWBits / 8 : kWRow;  // bytes of w's rows in LDS
-    static_assert(!kAcross || (kXBits == 8 && kWBits >= 4), "digits, and codes that the transposing reads know");
+    static_assert(!kAcross || kXBits == 8, "digits");
     constexpr int kXBytes = Shape::x_rows * kXRow, kWBytes = Shape::w_rows * kWRow, kStage = kXBytes + kWBytes;
-    constexpr int kXLoads = kXBytes / 1024 / Shape::waves, kWLoads = kWBytes / 1024 / Shape::waves;
-    static_assert(kXLoads * 1024 * Shape::waves == kXBytes && kWLoads * 1024 * Shape::waves == kWBytes, "whole loads per wave");
+    constexpr int kXLoads = kXBytes / 1024 / Shape::waves, kWCount = kWBytes / 1024, kWLoads = (kWCount + Shape::waves - 1) / Shape::waves;
+    static_assert(kXLoads * 1024 * Shape::waves == kXBytes && (kWCount % Shape::waves == 0 || Shape::waves % kWCount == 0),
+                  "whole loads per wave, or some waves load the same");
     static_assert(Shape::pieces % kPlanes == 0 && (kPlanes == 1 || kXBits == 8), "planes of a token in one wave");
     constexpr int kTokens = Shape::x_rows / kPlanes, kP = Shape::pieces;
     constexpr bool kNatural = kXBits != kWBits && !kAcross;  // (digits are written in the order that they meet)
@@ -109,10 +124,11 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
         x_base[i] = A.x + plane * A.plane_step + rt.row0 * A.ldx;
         x_off[i] = (uint32_t)(token < last ? token : last) * (uint32_t)A.ldx + x_piece[i] * 16;
     }
+    const int w_wave = kWCount < Shape::waves ? wave % kWCount : wave;
     w_base = A.w + rt.expert * A.w_step + (kAcross ? (int64_t)o0 * kWBits / 8 : (int64_t)o0 * A.ldw);
 #pragma unroll
     for (int i = 0; i < kWLoads; ++i) {
-        const int row = (i * Shape::waves + wave) * (1024 / kWLine) + lane / (kWLine / 16);
+        const int row = (i * Shape::waves + w_wave) * (1024 / kWLine) + lane / (kWLine / 16);
         if constexpr (kAcross) {
             const int piece = (lane % (kWLine / 16)) ^ across_turn<kWLine, kWBits>(row), last = (int)((int64_t)(A.n - o0) * kWBits / 128) - 1;
             w_piece[i] = row;
@@ -134,7 +150,7 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
         } else if constexpr (kAcross) {
             // rows behind the last: the last one (the digits there are 0)
             const int i = n - kXLoads, behind = s == stages - 1 ? s * 128 + w_piece[i] - (A.w_rows - 1) : 0;
-            load_to_lds(at + kXBytes + i * Shape::waves * 1024, w_off[i] - (behind > 0 ? behind * (uint32_t)A.ldw : 0u), w_base + (int64_t)s * 128 * A.ldw);
+            load_to_lds(at + kXBytes + (i * Shape::waves + w_wave - wave) * 1024, w_off[i] - (behind > 0 ? behind * (uint32_t)A.ldw : 0u), w_base + (int64_t)s * 128 * A.ldw);
         } else {
             const int i = n - kXLoads;
             const bool missing = w_tail && s == stages - 1 && w_piece[i] >= w_tail;
@@ -156,15 +172,16 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
     auto read_w = [&](int place, int n, int h, uint32_t (&v)[4][kWWords]) {
         const int j = n % 4;
         if constexpr (kAcross) {
-            const int rows = h * 16 + n / 4 * 8, word = (kWBits == 8 ? 4 : 2) * h + n / 4 * 2;
-            const int at = place * kStage + kXBytes + (kWBits == 8 ? across_at ^ (j * 16) : (across_at ^ (j / 2 * 16)) + j % 2 * 8) + rows * kWLine;
+            const int rows = h * 16 + n / 4 * 8, half = kWBits == 8 ? 0 : j % 2 * 8, piece = kWBits == 8 ? j : kWBits == 4 ? j / 2 : 0;
+            const int at = place * kStage + kXBytes + (across_at ^ (piece * 16)) + half + rows * kWLine;
+            const int to = kWBits == 2 ? 2 * j + h : j, word = kWBits == 8 ? 4 * h + n / 4 * 2 : kWBits == 4 ? 2 * h : 0;
             typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
             i32x2 q;
             if constexpr (kWBits == 8)
                 q = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(tile_lds + at));
             else
                 q = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)(tile_lds + at));
-            v[j][word] = (uint32_t)q[0]; v[j][word + 1] = (uint32_t)q[1];
+            v[to][word] = (uint32_t)q[0]; v[to][word + 1] = (uint32_t)q[1];
             return;
         }
         const uint8_t *p = tile_lds + place * kStage + kXBytes + (w_row + j * 4) * kWRow;
@@ -192,7 +209,7 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
     // the barrier the reads of 8 waves would hold up everyone's products.
     constexpr int kRing = kP % 4 == 0 ? 4 : 3;
     static_assert(kP % kRing == 0 && kP >= 4, "the ring's places are the same in every stage");
-    constexpr int kWTurns = kAcross || kWWords == 8 ? 2 : 1, kWEach = kAcross && kWBits == 8 ? 8 : 4;
+    constexpr int kWTurns = kAcross || kWWords == 8 ? 2 : 1, kWEach = !kAcross || kWBits == 4 ? 4 : kWBits;
     constexpr int kXReads = kXWords / 4, kWReads = kWTurns * kWEach;  // of a piece of x; of all of w
     constexpr int kFirst = kWReads + 2 * kXReads;  // reads that a stage starts from
     i32x4 acc[kP][4] = {};
@@ -214,7 +231,12 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
 #pragma unroll
         for (int h = 0; h < kSteps; ++h)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) a[h][j] = step_codes<kWBits, kNatural>(wv[j], h);
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (kAcross && kWBits == 2)
+                    a[h][j] = pair_codes(wv[j / 2 * 2 + h], j % 2);
+                else
+                    a[h][j] = step_codes<kWBits, kNatural>(wv[j], h);
+            }
         i32x4 b = step_codes<kXBits, kNatural>(xv[0], 0);
 #pragma unroll
         for (int q = 0; q < kSteps * kP; ++q) {
@@ -286,24 +308,26 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
     stage(s, place, 0, wv[0], wv[1], std::integral_constant<int, 0>{});
 
     if constexpr (kAcross) {  // a gradient has no scales and no bias of the channels
-        const int o = o0 + wave_n * 64 + g * 4;
+        constexpr int kRun = kWBits == 2 ? 8 : 4, kRuns = 16 / kRun;  // neighbouring channels of a lane
+        const int o = o0 + wave_n * 64 + g * kRun;
 #pragma unroll
         for (int i = 0; i < kP / kPlanes; ++i) {
             const int64_t t = rt.row0 + (wave_t * (kP / kPlanes) + i) * 16 + r16;
             if (t >= rt.row_end) continue;
             const float s = load_scale(A.xs, t, A.xs_f16) * A.factor;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (o + 16 * j >= A.n) continue;
-                float v[4];
+            for (int j = 0; j < kRuns; ++j) {
+                const int first = o + 4 * kRun * j;
+                if (first >= A.n) continue;
+                float v[kRun];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
+                for (int r = 0; r < kRun; ++r) {
                     int part[kPlanes];
 #pragma unroll
-                    for (int p = 0; p < kPlanes; ++p) part[p] = acc[i * kPlanes + p][j][r];
+                    for (int p = 0; p < kPlanes; ++p) part[p] = kWBits == 2 ? acc[i * kPlanes + p][2 * j + r % 2][r / 2] : acc[i * kPlanes + p][j][r % 4];
                     v[r] = joined<kPlanes>(part) * s;
                 }
-                store_results<4>(A, t * A.ldy + o + 16 * j, v, A.n - o - 16 * j);
+                store_results<kRun>(A, t * A.ldy + first, v, A.n - first);
             }
         }
         return;

@@ -19,7 +19,9 @@ static hipError_t launch(const LinearArgs &A, int planes, LinearTile tile, hipSt
 
 hipError_t launch_linear_tile_across(const LinearArgs &A, int wbits, int planes, LinearTile tile, hipStream_t stream)
 {
-    return wbits == 8 ? launch<8>(A, planes, tile, stream) : launch<4>(A, planes, tile, stream);
+    if (wbits == 8) return launch<8>(A, planes, tile, stream);
+    if (wbits == 4) return launch<4>(A, planes, tile, stream);
+    return launch<2>(A, planes, tile, stream);
 }
 
 }  // namespace bq

@@ -481,10 +481,12 @@ def _check_bwd(T, N, K, experts, wbits, dtype, scale, seed, pad_w=0, pad_dx=0, s
 
 # as many rows as make it worth while to read the weights as they lie: the sum's length and the inputs around tiles' ends, the smallest sums
 ACROSS = [(19, 10, 20000, 0, 0), (300, 520, 2080, 0, 16), (115, 10, 20000, 3, 0), (150, 10, 20000, 3, 32), (4100, 10, 544, 50, 0), (700, 1100, 1568, 0, 48),
-          (1000, 130, 672, 3, 0), (255, 777, 992, 0, 0), (2040, 384, 256, 0, 16), (3000, 1, 288, 0, 0), (999, 128, 2336, 3, 0), (513, 129, 1056, 0, 0)]
+          (1000, 130, 672, 3, 0), (255, 777, 992, 0, 0), (2040, 384, 256, 0, 16), (3000, 1, 288, 0, 0), (999, 128, 2336, 3, 0), (513, 129, 1056, 0, 0),
+          (300, 520, 2112, 0, 16), (700, 1100, 1600, 0, 48), (1000, 130, 704, 3, 0), (255, 777, 1024, 0, 0), (4100, 10, 576, 50, 0), (19, 10, 20032, 0, 0),
+          (115, 10, 20032, 3, 0), (150, 10, 20032, 3, 32), (600, 1024, 4096, 0, 0), (350, 640, 1536, 0, 0)]
 
 
-@pytest.mark.parametrize("wbits", [8, 4])
+@pytest.mark.parametrize("wbits", [8, 4, 2])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("T,N,K,experts,pad_w", ACROSS)
 def test_bwd_on_weights_as_they_lie(T, N, K, experts, pad_w, dtype, wbits):

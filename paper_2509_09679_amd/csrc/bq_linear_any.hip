@@ -55,7 +55,7 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinearArgs A, int xbits
     for (int j = 0; j < 2; ++j) {
         const int64_t t = rt.row0 + tt + 16 * j + r16;
         if (t >= rt.row_end) continue;
-        const float xs = load_scale(A.xs, t, A.xs_f16) * A.factor;
+        const float xs = load_scale(A.xs, t, A.xs_f16);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinearArgs A, int xbits
                 const int o = o0 + to + 16 * i + (lane >> 4) * 4 + r;
                 if (o >= A.n) continue;
                 const int64_t at = (int64_t)rt.expert * A.n + o;
-                float v = (float)acc[i][j][r] * xs * load_scale(A.ws, at, A.ws_f16);
+                float v = (float)acc[i][j][r] * A.factor * xs * load_scale(A.ws, at, A.ws_f16);
                 if (A.bias) v += load_row_value(A.bias, at, A.dtype);
                 store_row_value(A.y, t * A.ldy + o, A.dtype, v);
             }

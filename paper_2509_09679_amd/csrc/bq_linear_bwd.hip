@@ -71,13 +71,13 @@ __device__ __forceinline__ RowFactor row_factor(uint32_t amax_bits)
     constexpr float kMost = kPlanes == 3 ? 8355711.0f : 32639.0f;
     const bool finite = amax_bits < 0x7F800000u;
     const float amax = __uint_as_float(amax_bits);
-    // rows of tiny entries are lifted first: m / amax has to be a float32 number
+    // rows of tiny entries are lifted first: m / amax and amax / m have to be float32 numbers with all their digits; the factor's sign says so
     RowFactor f;
     f.lift = amax < 0x1p-60f ? 0x1p60f : 1.0f;
     const float top = amax * f.lift;
     const bool some = finite && top >= 0x1p-60f;  // (below 2^-120 the row counts as 0)
     f.inv = some ? kMost / top : 0.0f;
-    f.factor = !finite ? __uint_as_float(0x7FC00000u) : some ? (top / kMost) / f.lift : 0.0f;
+    f.factor = !finite ? __uint_as_float(0x7FC00000u) : some ? (f.lift != 1.0f ? -top : top) / kMost : 0.0f;
     return f;
 }
 

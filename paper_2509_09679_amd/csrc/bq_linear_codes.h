@@ -84,6 +84,26 @@ __device__ __forceinline__ float joined(const int (&sum)[kPlanes])
     if constexpr (kPlanes == 3) return (float)__builtin_fma((double)sum[0], 65536.0, __builtin_fma((double)sum[1], 256.0, (double)sum[2]));
 }
 
+// What a token's sums are multiplied with.  The fields' factor, a power of two, goes to the sum, where it is exact: a scale near float32's
+// smallest would lose digits to it.  A gradient's row factor is negative if the row was lifted by 2^60 (bq_linear_bwd.hip).
+struct TokenScale {
+    float fields, scale, lower;
+};
+
+template <int kPlanes>
+__device__ __forceinline__ TokenScale token_scale(float scale, float fields)
+{
+    if constexpr (kPlanes == 1) return TokenScale{fields, scale, 1.0f};
+    return TokenScale{fields, fabsf(scale), scale < 0.0f ? 0x1p-60f : 1.0f};
+}
+
+template <int kPlanes>
+__device__ __forceinline__ float scaled(const int (&sum)[kPlanes], const TokenScale &s)
+{
+    const float v = joined<kPlanes>(sum) * s.fields * s.scale;
+    return kPlanes == 1 ? v : v * s.lower;
+}
+
 // scales and bias of some channels or tokens: every type's loads in a branch of its own, so that they are in flight together
 template <int kCount>
 __device__ __forceinline__ void load_scales(const void *p, int f16, const int64_t (&at)[kCount], float (&s)[kCount])

@@ -162,7 +162,7 @@ __global__ __launch_bounds__((64 * RowsShape<kXBits, kWBits, kPlanes, kBlocks, k
             const int64_t t = row0 + 16 * block + r16;
             const int o = o0 + 16 * col + 4 * g;
             if (t >= row_b || o >= A.n) continue;
-            const float xs = load_scale(A.xs, t, A.xs_f16) * A.factor;
+            const TokenScale xs = token_scale<kPlanes>(load_scale(A.xs, t, A.xs_f16), A.factor);
             int64_t at[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) at[r] = (int64_t)expert * A.n + (o + r < A.n ? o + r : A.n - 1);
@@ -174,7 +174,7 @@ __global__ __launch_bounds__((64 * RowsShape<kXBits, kWBits, kPlanes, kBlocks, k
                 int part[kPlanes];
 #pragma unroll
                 for (int p = 0; p < kPlanes; ++p) part[p] = sum[p][r];
-                v[r] = joined<kPlanes>(part) * xs;
+                v[r] = scaled<kPlanes>(part, xs);
                 if (A.ws) v[r] *= ws[r];
                 if (A.bias) v[r] += bias[r];
             }

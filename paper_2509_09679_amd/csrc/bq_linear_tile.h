@@ -321,7 +321,7 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
         for (int i = 0; i < kP / kPlanes; ++i) {
             const int64_t t = rt.row0 + (wave_t * (kP / kPlanes) + i) * 16 + r16;
             if (t >= rt.row_end) continue;
-            const float s = load_scale(A.xs, t, A.xs_f16) * A.factor;
+            const TokenScale s = token_scale<kPlanes>(load_scale(A.xs, t, A.xs_f16), A.factor);
 #pragma unroll
             for (int j = 0; j < kRuns; ++j) {
                 const int first = o + 4 * kRun * j;
@@ -333,7 +333,7 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
 #pragma unroll
                     for (int p = 0; p < kPlanes; ++p)
                         part[p] = kWBits == 2 ? acc[i * kPlanes + p][2 * j + r % 2][r / 2] : acc[i * kPlanes + p][j][r % 4];
-                    v[r] = joined<kPlanes>(part) * s;
+                    v[r] = scaled<kPlanes>(part, s);
                 }
                 store_results<kRun>(A, t * A.ldy + first, v, A.n - first);
             }
@@ -359,14 +359,14 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
 #pragma unroll
     for (int i = 0; i < kOut; ++i) {
         if (t0 + 16 * i >= rt.row_end) continue;
-        const float s = xs[i] * A.factor;
+        const TokenScale s = token_scale<kPlanes>(xs[i], A.factor);
         float v[16];
 #pragma unroll
         for (int c = 0; c < 16; ++c) {
             int part[kPlanes];
 #pragma unroll
             for (int p = 0; p < kPlanes; ++p) part[p] = acc[i * kPlanes + p][c >> 2][c & 3];
-            v[c] = joined<kPlanes>(part) * s;
+            v[c] = scaled<kPlanes>(part, s);
             if (A.ws) v[c] *= ws[c];
             if (A.bias) v[c] += bias[c];
         }

@@ -125,6 +125,17 @@ def test_linear_fwd_scales_carry_nan_and_zero():
     assert torch.isnan(y[3]).all() and (y[5] == 0).all() and (y[:3, 7] == 0).all() and torch.isfinite(y[4]).all()
 
 
+@pytest.mark.parametrize("bits", BITS)
+@pytest.mark.parametrize("T,N,K", [(3, 40, 128), (70, 200, 512), (300, 264, 256), (20, 30, 51)])
+def test_linear_fwd_smallest_scales(T, N, K, bits):
+    # scales of rows down to float32's smallest normal number, the smallest that the quantisers write
+    L = Layer(np.random.default_rng([T, N, K, *bits]), T, N, K, xbits=bits[0], wbits=bits[1], dtype="f32")
+    L.xs = L.xs * 0 + 2.0 ** -126 * (1 + torch.rand(T, device=DEV))
+    L.ws = 1 + torch.rand(N, device=DEV)
+    want, size = lu.reference_fwd(L.qx, L.xs, L.qw, L.ws, None, [0, T])
+    lu.check(lu.f64(L.forward()), want, 5 * 2.0 ** -24 * size + 2.0 ** -148, f"{bits}")
+
+
 GROUPS = [
     (40, [0, 40]),
     (40, [0, 0, 40, 40]),
@@ -234,6 +245,22 @@ def test_bwd_special_rows(dtype):
     keep = [3, 4, 6, 7, 8]
     lu.check(dx[keep], want[keep], lu.bound_bwd(want, weight, top, dtype)[keep], "rows")
     assert np.isfinite(dx[5]).all() and (np.abs(dx[5] - want[5]) <= 2.0 ** -119 * weight[5]).all()
+
+
+@pytest.mark.parametrize("wbits", [8, 4, 2])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,K", [(5, 64, 48), (40, 200, 96), (300, 520, 2112)])
+def test_bwd_of_tiny_rows(T, N, K, dtype, wbits):
+    # row by row from 2^-60 to 2^-118, the last binade above the one that may count as 0
+    rng = np.random.default_rng([T, N, K, wbits])
+    L = Layer(rng, T, N, K, wbits=wbits, dtype=dtype)
+    L.ws = 1 + torch.rand(N, device=DEV)
+    g = rng.uniform(-1, 1, size=(T, N))
+    g[:, 0] = 1
+    dy = torch.from_numpy(g * 2.0 ** -np.linspace(60, 118, T).round()[:, None]).to(TORCH[dtype]).to(DEV)
+    want, weight, top = lu.reference_bwd(dy, L.qw, L.ws, [0, T])
+    f32 = (0.5 / lu.QMAX[3 if dtype == "f32" else 2] + 5 * 2.0 ** -24) * top[:, None] * weight + 2 * 2.0 ** -24 * np.abs(want)
+    lu.check(lu.f64(L.backward(dy)), want, f32 + (lu.half_step(dtype) * (np.abs(want) + f32) if dtype != "f32" else 0) + 2.0 ** -148, "dx")
 
 
 # ---- streams, graphs, a layer as it is used --------------------------------------------------------------

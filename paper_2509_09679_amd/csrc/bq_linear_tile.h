@@ -314,14 +314,22 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
     }
     stage(s, place, 0, wv[0], wv[1], std::integral_constant<int, 0>{});
 
+    // (all loads in flight together: one after another, a token's scale at a time, they were a third of the time behind the last stage)
+    constexpr int kOut = kP / kPlanes;
+    const int64_t t0 = rt.row0 + wave_t * kOut * 16 + r16;
+    int64_t token[kOut];
+    float xs[kOut];
+#pragma unroll
+    for (int i = 0; i < kOut; ++i) token[i] = t0 + 16 * i < rt.row_end ? t0 + 16 * i : rt.row_end - 1;
+    token_scales(A, token, xs);
     if constexpr (kAcross) {  // a gradient has no scales and no bias of the channels
         constexpr int kRun = kWBits == 2 ? 8 : 4, kRuns = 16 / kRun;  // neighbouring channels of a lane
         const int o = o0 + wave_n * 64 + g * kRun;
 #pragma unroll
-        for (int i = 0; i < kP / kPlanes; ++i) {
-            const int64_t t = rt.row0 + (wave_t * (kP / kPlanes) + i) * 16 + r16;
+        for (int i = 0; i < kOut; ++i) {
+            const int64_t t = t0 + 16 * i;
             if (t >= rt.row_end) continue;
-            const TokenScale s = token_scale<kPlanes>(load_scale(A.xs, t, A.xs_f16), A.factor);
+            const TokenScale s = token_scale<kPlanes>(xs[i], A.factor);
 #pragma unroll
             for (int j = 0; j < kRuns; ++j) {
                 const int first = o + 4 * kRun * j;
@@ -348,14 +356,6 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
     for (int c = 0; c < 16; ++c) channel[c] = (int64_t)rt.expert * A.n + (o + c < A.n ? o + c : A.n - 1);
     channel_scales(A, channel, ws);
     channel_bias(A, channel, bias);
-    // (all loads in flight together: one after another, a token's scale at a time, they were a third of the time behind the last stage)
-    constexpr int kOut = kP / kPlanes;
-    const int64_t t0 = rt.row0 + wave_t * kOut * 16 + r16;
-    int64_t token[kOut];
-    float xs[kOut];
-#pragma unroll
-    for (int i = 0; i < kOut; ++i) token[i] = t0 + 16 * i < rt.row_end ? t0 + 16 * i : rt.row_end - 1;
-    token_scales(A, token, xs);
 #pragma unroll
     for (int i = 0; i < kOut; ++i) {
         if (t0 + 16 * i >= rt.row_end) continue;

@@ -214,7 +214,7 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
     // by one between the products (four of them each), in the order written here: a wave issues in order, and in one burst behind
     // the barrier the reads of 8 waves would hold up everyone's products.
     constexpr int kRing = kP % 4 == 0 ? 4 : 3;
-    static_assert(kP % kRing == 0 && kP >= 4, "the ring's places are the same in every stage");
+    static_assert(kP % kRing == 0, "the ring's places are the same in every stage");
     constexpr int kWTurns = kAcross || kWWords == 8 ? 2 : 1, kWEach = !kAcross || kWBits == 4 ? 4 : kWBits;
     constexpr int kXReads = kXWords / 4, kWReads = kWTurns * kWEach;  // of a piece of x; of all of w
     constexpr int kFirst = kWReads + 2 * kXReads;  // reads that a stage starts from
@@ -395,6 +395,6 @@ typedef TileShape<2, 4, 4, 160> TileMiddle;  // 128 x 256
 typedef TileShape<2, 2, 4, 80> TileSmall;    // 128 x 128, two workgroups per compute unit
 typedef TileShape<2, 2, 4, 160> TileDeep;    // 128 x 128, one of them with all of the LDS (8-bit codes: four stages instead of two)
 typedef TileShape<4, 2, 6, 160> TileLarge3;  // 384 x 128, for three planes
-typedef TileShape<2, 2, 6, 160> TileDeep3;   // 192 x 128
+typedef TileShape<4, 2, 3, 160> TileDeep3;   // 192 x 128
 
 }  // namespace bq

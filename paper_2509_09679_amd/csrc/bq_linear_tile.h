@@ -213,14 +213,14 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
     // kDepth further on; the products of the last two pieces cover the first reads of the next stage.  Reads and loads stand one
     // by one between the products (four of them each), in the order written here: a wave issues in order, and in one burst behind
     // the barrier the reads of 8 waves would hold up everyone's products.
-    constexpr int kRing = kP % 4 == 0 ? 4 : 3;
+    constexpr int kRing = kP == 2 ? 2 : kP % 4 == 0 ? 4 : 3, kX = kP == 2 ? 2 : 1;  // (two pieces are all read ahead: x alternates like w)
     static_assert(kP % kRing == 0, "the ring's places are the same in every stage");
     constexpr int kWTurns = kAcross || kWWords == 8 ? 2 : 1, kWEach = !kAcross || kWBits == 4 ? 4 : kWBits;
     constexpr int kXReads = kXWords / 4, kWReads = kWTurns * kWEach;  // of a piece of x; of all of w
     constexpr int kFirst = kWReads + 2 * kXReads;  // reads that a stage starts from
     i32x4 acc[kP][4] = {};
-    uint32_t wv[2][4][kWWords], xv[kRing][kXWords];  // (w's codes alternate: in one array every stage began by copying them)
-    auto first_read = [&](int place, int n, uint32_t (&wv)[4][kWWords]) {
+    uint32_t wv[2][4][kWWords], xv[kX][kRing][kXWords];  // (w's codes alternate: in one array every stage began by copying them)
+    auto first_read = [&](int place, int n, uint32_t (&wv)[4][kWWords], uint32_t (&xv)[kRing][kXWords]) {
         // w's first halves, x's first piece, w's other halves, x's second piece
         if (n < kWEach)
             read_w(place, n, 0, wv);
@@ -232,7 +232,8 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
             read_x(place, 1, n - kWReads - kXReads, xv[1]);
     };
     // LEFT: 2 in the ring's steady state, 1 behind the last load, 0 the last
-    auto stage = [&](int s, int place, int next_place, const uint32_t (&wv)[4][kWWords], uint32_t (&wn)[4][kWWords], auto LEFT) {
+    auto stage = [&](int s, int place, int next_place, const uint32_t (&wv)[4][kWWords], uint32_t (&wn)[4][kWWords], uint32_t (&xv)[kRing][kXWords],
+                     uint32_t (&xn)[kRing][kXWords], auto LEFT) {
         constexpr int left = decltype(LEFT)::value;
         i32x4 a[kSteps][4];
 #pragma unroll
@@ -265,7 +266,7 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
                     for (int n = (q - kTurn) * kLoads / kOver; n < (q - kTurn + 1) * kLoads / kOver; ++n) load(s + kDepth, place, n);
                 }
 #pragma unroll
-                for (int n = (q - kTurn) * kFirst / kOver; n < (q - kTurn + 1) * kFirst / kOver; ++n) first_read(next_place, n, wn);
+                for (int n = (q - kTurn) * kFirst / kOver; n < (q - kTurn + 1) * kFirst / kOver; ++n) first_read(next_place, n, wn, xn);
             }
             i32x4 next = b;
             if (q + 1 < kSteps * kP) next = step_codes<kXBits, kNatural>(xv[((q + 1) / kSteps) % kRing], (q + 1) % kSteps);
@@ -286,33 +287,37 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
         asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
     clear_tail(0, 0);
 #pragma unroll
-    for (int n = 0; n < kFirst; ++n) first_read(0, n, wv[0]);
+    for (int n = 0; n < kFirst; ++n) first_read(0, n, wv[0], xv[0]);
     auto after = [&](int place) { return place + 1 == kDepth ? 0 : place + 1; };
     auto even_again = [&] {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int v = 0; v < kWWords; ++v) wv[0][j][v] = wv[1][j][v];
+#pragma unroll
+        for (int i = 0; i < kRing; ++i)
+#pragma unroll
+            for (int v = 0; v < kXWords; ++v) xv[0][i][v] = xv[kX - 1][i][v];
     };
     int s = 0, place = 0;
     for (; s + kDepth + 1 < stages; s += 2) {
         const int second = after(place), third = after(second);
-        stage(s, place, second, wv[0], wv[1], std::integral_constant<int, 2>{});
-        stage(s + 1, second, third, wv[1], wv[0], std::integral_constant<int, 2>{});
+        stage(s, place, second, wv[0], wv[1], xv[0], xv[kX - 1], std::integral_constant<int, 2>{});
+        stage(s + 1, second, third, wv[1], wv[0], xv[kX - 1], xv[0], std::integral_constant<int, 2>{});
         place = third;
     }
     if (s + kDepth < stages) {
-        stage(s, place, after(place), wv[0], wv[1], std::integral_constant<int, 2>{});
+        stage(s, place, after(place), wv[0], wv[1], xv[0], xv[kX - 1], std::integral_constant<int, 2>{});
         even_again();
         place = after(place);
         ++s;
     }
     for (; s + 1 < stages; ++s) {
-        stage(s, place, after(place), wv[0], wv[1], std::integral_constant<int, 1>{});
+        stage(s, place, after(place), wv[0], wv[1], xv[0], xv[kX - 1], std::integral_constant<int, 1>{});
         even_again();
         place = after(place);
     }
-    stage(s, place, 0, wv[0], wv[1], std::integral_constant<int, 0>{});
+    stage(s, place, 0, wv[0], wv[1], xv[0], xv[kX - 1], std::integral_constant<int, 0>{});
 
     // (all loads in flight together: one after another, a token's scale at a time, they were a third of the time behind the last stage)
     constexpr int kOut = kP / kPlanes;
@@ -393,7 +398,7 @@ typedef TileShape<2, 4, 8, 160> TileLarge;   // 256 x 256
 typedef TileShape<2, 4, 6, 160> TileTall;    // 192 x 256, for 8-bit codes
 typedef TileShape<2, 4, 4, 160> TileMiddle;  // 128 x 256
 typedef TileShape<2, 2, 4, 80> TileSmall;    // 128 x 128, two workgroups per compute unit
-typedef TileShape<2, 2, 4, 160> TileDeep;    // 128 x 128, one of them with all of the LDS (8-bit codes: four stages instead of two)
+typedef TileShape<4, 2, 2, 160> TileDeep;    // 128 x 128, one of them with all of the LDS (8-bit codes: four stages instead of two)
 typedef TileShape<4, 2, 6, 160> TileLarge3;  // 384 x 128, for three planes
 typedef TileShape<4, 2, 3, 160> TileDeep3;   // 192 x 128
 

@@ -33,17 +33,17 @@ double pieces(const LinearArgs &A, int rows)
 }
 
 // What a kernel takes, in us.  The constants below are fits to a sweep of all kernels (1 .. 8192 tokens, (K, N) from (1024, 2048) to
-// (11008, 4096), (8192, 8192) and (4096, 32000), codes of 8, 4 and 2 bits, digits): what they choose is within 2 % of the best of the
-// sweep's kernels on average, within 12 % at 93 % of its 858 points.  Measured, 8-bit codes 4096 -> 4096, us:
+// (11008, 4096), (8192, 8192) and (4096, 32000), codes of 8, 4 and 2 bits, digits): what they choose is within 2.5 % of the best of the
+// sweep's kernels on average.  Measured, 8-bit codes 4096 -> 4096, us:
 //   tokens          1    16    32    64   128   256   512  1024  2048  4096  8192
-//   1x1           6.0   6.6   8.6  12.6  20.7  36.1  67.3   112
-//   2x2           6.4   6.9   7.5   7.5  11.0  18.0  30.4  52.9
-//   4x2           7.9   8.2   8.8   9.7  10.0  17.4  32.1  58.2
-//   128 x 128 deep 16    17    17    19    20    21    21    22    41    85   184
-//   128 x 128      23    24    24    26    26    27    28    26    36    70   147
-//   128 x 256      22    23    24    26    28    28    28    27    34    68   141
-//   192 x 256                                       41    42    37    42    84   139
-//   256 x 256      38    39    40    41    44    46    48    45    47    60   120
+//   1x1           5.9   6.5   8.5  12.6  20.5  35.7  67.9   115
+//   2x2           6.4   6.9   7.4   7.4  10.9  18.0  30.9  53.9
+//   4x2           7.8   8.1   8.6   9.5   9.7  17.3  31.7  57.9
+//   128 x 128 deep 16    16    17    18    19    20    20    22    42    85   187
+//   128 x 128      23    25    26    26    27    27    28    26    36    71   152
+//   128 x 256      22    23    24    26    28    28    29    27    35    71   145
+//   192 x 256      32    34    35    36    38    38    40    38    40    83   138
+//   256 x 256      38    40    40    41    44    47    48    45    50    62   122
 
 // The weights' bytes, at what a kernel that has to wait for them reaches.
 double weights_us(const LinearArgs &A, int wbits)
@@ -91,16 +91,19 @@ Choice choose(const LinearArgs &A, int xbits, int wbits, int planes, bool across
         }
     }
     if (planes < 3) {
-        // 128 x 128: two workgroups on a compute unit, or one; packed codes have the same stages either way
-        const bool packed = xbits < 8 || wbits < 8;
         tiles(kTileLarge, tile_us(A, wbits, planes, 256, 256, kCUs, 5.35, 1.50));
         if (xbits == 8) tiles(kTileTall, tile_us(A, wbits, planes, 192, 256, kCUs, 4.3, 1.33));
         tiles(kTileMiddle, tile_us(A, wbits, planes, 128, 256, kCUs, 3.1, 0.93));
         tiles(kTileSmall, tile_us(A, wbits, planes, 128, 128, 2.0 * kCUs, 4.2, 0.93));
-        tiles(packed ? kTileSmall : kTileDeep, tile_us(A, wbits, planes, 128, 128, kCUs, 4.4, 0.66));
+        // one on a compute unit: eight waves with all of its LDS (512 tokens, 4096 -> 4096: 20.3 us, four waves 22.3 us), but packed
+        // weights, which every wave along the tokens unpacks for itself, stay with four (22.1, eight waves 23.0 us)
+        if (wbits == 8)
+            tiles(kTileDeep, tile_us(A, wbits, planes, 128, 128, kCUs, 3.5, 0.52));
+        else
+            tiles(kTileSmall, tile_us(A, wbits, planes, 128, 128, kCUs, 4.4, 0.66));
     } else {
         tiles(kTileLarge, tile_us(A, wbits, 3, 384, 128, kCUs, 4.7, 1.24));
-        tiles(kTileDeep, tile_us(A, wbits, 3, 192, 128, kCUs, 5.8, 0.71));
+        tiles(kTileDeep, tile_us(A, wbits, 3, 192, 128, kCUs, 5.0, 0.62));
     }
     return c;
 }

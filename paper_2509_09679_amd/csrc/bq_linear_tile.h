@@ -159,7 +159,7 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
         } else {
             const int i = n - kXLoads;
             const bool missing = w_tail && s == stages - 1 && w_piece[i] >= w_tail;
-            load_to_lds(at + kXBytes + i * Shape::waves * 1024, missing ? w_off[i] - w_piece[i] * 16 : w_off[i], w_base + (int64_t)s * kWRow);
+            load_to_lds(at + kXBytes + (i * Shape::waves + w_wave - wave) * 1024, missing ? w_off[i] - w_piece[i] * 16 : w_off[i], w_base + (int64_t)s * kWRow);
         }
     };
 
@@ -398,7 +398,7 @@ typedef TileShape<2, 4, 8, 160> TileLarge;   // 256 x 256
 typedef TileShape<2, 4, 6, 160> TileTall;    // 192 x 256, for 8-bit codes
 typedef TileShape<2, 4, 4, 160> TileMiddle;  // 128 x 256
 typedef TileShape<2, 2, 4, 80> TileSmall;    // 128 x 128, two workgroups per compute unit
-typedef TileShape<4, 2, 2, 160> TileDeep;    // 128 x 128, one of them with all of the LDS (8-bit codes: four stages instead of two)
+typedef TileShape<4, 2, 2, 160> TileDeep;    // 128 x 128, one of them with eight waves and all of the LDS
 typedef TileShape<4, 2, 6, 160> TileLarge3;  // 384 x 128, for three planes
 typedef TileShape<4, 2, 3, 160> TileDeep3;   // 192 x 128
 

@@ -8,6 +8,9 @@ static hipError_t launch(const LinearArgs &A, LinearTile tile, hipStream_t strea
 {
     if (tile == kTileLarge) return launch_tile<4, kWBits, 1, TileLarge>(A, stream);
     if (tile == kTileMiddle) return launch_tile<4, kWBits, 1, TileMiddle>(A, stream);
+    if constexpr (kWBits == 8) {
+        if (tile == kTileDeep) return launch_tile<4, 8, 1, TileDeep>(A, stream);
+    }
     return launch_tile<4, kWBits, 1, TileSmall>(A, stream);
 }
 

@@ -10,9 +10,9 @@
 // with packed codes one read then serves both.  Row i of the first operand's piece j is channel 16 (i / 4) + 4 j + i % 4 of the wave's 64:
 // a lane ends with 16 consecutive channels of one token.
 //
-// Bound by the matrix cores at the clock that the power limit leaves them, and by what part of the last round of tiles is full.  4-bit
-// codes, 16384 tokens, 8192 -> 8192: 745 us, 2.95 POP/s, where a loop of the same instruction on random registers reaches 4.2; 8-bit codes,
-// 1777 tokens, 4096 -> 11008: 80 us, 2.0 POP/s; a gradient's two planes, 2048 tokens, 4096 -> 4096: 58 us, 2.36 POP/s.
+// Bound by the matrix cores (60 .. 65 % busy) at the clock that the power limit leaves them, by what part of the last round of tiles is full,
+// and with packed codes by the vector instructions that unpack them, 2.7 per matrix instruction.  4-bit codes, 16384 tokens, 8192 -> 8192: 745 us, 2.95 POP/s, where a loop of the same instruction on random registers reaches 4.2; 8-bit codes,
+// 1777 tokens, 4096 -> 11008: 80 us, 2.0 POP/s; a gradient's two planes, 2048 tokens, 4096 -> 4096: 57.5 us, 2.4 POP/s.
 #pragma once
 
 #include <type_traits>
@@ -400,6 +400,6 @@ typedef TileShape<2, 4, 4, 160> TileMiddle;  // 128 x 256
 typedef TileShape<2, 2, 4, 80> TileSmall;    // 128 x 128, two workgroups per compute unit
 typedef TileShape<4, 2, 2, 160> TileDeep;    // 128 x 128, one of them with eight waves and all of the LDS
 typedef TileShape<4, 2, 6, 160> TileLarge3;  // 384 x 128, for three planes
-typedef TileShape<4, 2, 3, 160> TileDeep3;   // 192 x 128
+typedef TileShape<4, 2, 3, 160> TileDeep3;   // 192 x 128 (by four waves 333 tokens of 4096 -> 5120 took 30.7 us instead of 28.5)
 
 }  // namespace bq

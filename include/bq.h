@@ -227,7 +227,7 @@ bq_status bq_quantiser_grad(const void *v, const void *vq, float *g, const float
  *   x     : [rows][ld_x] of dtype (bq_dtype), cols used elements per row, ld_x >= cols (elements)
  *   codes : [rows][ld_codes] bytes, ld_codes >= cols; bytes behind the columns are left as they were
  *   scales: [rows] of scale_dtype (BQ_F32 or BQ_F16)
- * 0 <= rows < 2^31, 1 <= cols <= 2^24, rows * max(ld_x, ld_codes) <= 2^44. */
+ * The outputs must not overlap x.  0 <= rows < 2^31, 1 <= cols <= 2^24, rows * max(ld_x, ld_codes) <= 2^44. */
 bq_status bq_rows_quant8(const void *x, int64_t rows, int32_t cols, int64_t ld_x, int32_t dtype, int8_t *codes,
                          int64_t ld_codes, void *scales, int32_t scale_dtype, void *stream);
 
@@ -265,7 +265,7 @@ bq_status bq_linear_fwd(const void *x, const void *xscale, const void *w, const 
  * off by at most 2^-15.9 or 2^-21.6 of that largest one, and the sums are exact.  Rows whose entries are all below
  * 2^-120 give 0; a row with an infinity or a NaN in dy * wscale gives NaN throughout.
  *   dy: [rows][ld_y], dx: [rows][ld_x], both of dtype; workspace: at least the queried size, 256-byte aligned, its contents
- *   on entry are ignored.  dx must not overlap dy. */
+ *   on entry are ignored; calls that may run at once need one each.  dx must not overlap the inputs. */
 size_t bq_linear_bwd_workspace_bytes(const bq_linear *desc); /* 0 if the descriptor is invalid */
 bq_status bq_linear_bwd(const void *dy, const void *w, const void *wscale, void *dx, void *workspace,
                         size_t workspace_bytes, const bq_linear *desc, void *stream);

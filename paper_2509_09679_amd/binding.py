@@ -394,22 +394,18 @@ def _torch_types(code: int):
 def bq_rows_quant8(x, codes, scales, stream=None) -> None:
     """x: [rows, cols] of any row type, codes: int8 [rows, cols], both with a contiguous last dimension; scales: [rows], float32 or
     float16."""
-    rows, cols = x.shape
-    if rows > 1:
-        ld_x, step_x = x.stride()
-        ld_codes, step_codes = codes.stride()
-        _require(step_x == step_codes == 1 or cols == 1, 2, "bq_rows_quant8: the last dimension must be contiguous")
-    else:
-        ld_x = ld_codes = cols
-        _require(cols <= 1 or x.numel() == 0 or x.stride(1) == codes.stride(1) == 1, 2, "bq_rows_quant8: the last dimension must be contiguous")
-    if codes.shape != x.shape:
-        raise BqError(2, "bq_rows_quant8: codes and x differ in shape")
+    shape, (ld_x, step_x), (ld_codes, step_codes) = x.shape, x.stride(), codes.stride()
+    rows, cols = shape
     here, values = _here(), _ROW_TYPES or _row_types()
     x_code, scale_code = values.get(x.dtype, -1), values.get(scales.dtype, -1)
-    if not (x.get_device() == codes.get_device() == scales.get_device() == here and x_code >= 0 and 0 <= scale_code <= BQ_F16
-            and codes.dtype in _torch_types(-1) and scales.numel() >= rows and scales.is_contiguous()):
+    if not (step_x == step_codes == 1 and codes.shape == shape and x.get_device() == codes.get_device() == scales.get_device() == here
+            and x_code >= 0 and 0 <= scale_code <= BQ_F16 and codes.dtype in _torch_types(-1) and scales.numel() >= rows and scales.is_contiguous()):
+        _require(step_x == step_codes == 1 or cols == 1 or x.numel() == 0, 2, "bq_rows_quant8: the last dimension must be contiguous")
+        _require(codes.shape == shape, 2, "bq_rows_quant8: codes and x differ in shape")
         _refuse_tensors("bq_rows_quant8", (("x", x, tuple(values), 0, False), ("codes", codes, _torch_types(-1), 0, False),
                                            ("scales", scales, _torch_types(BQ_F32) + _torch_types(BQ_F16), rows, True)))
+    if rows <= 1:  # (a tensor of one row has no stride of its own)
+        ld_x = ld_codes = cols
     _check((_CALLS or _calls()).rows_quant8(x, rows, cols, ld_x, x_code, codes, ld_codes, scales, scale_code, _stream_ptr(stream)))
 
 

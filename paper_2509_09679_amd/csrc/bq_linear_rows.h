@@ -4,7 +4,8 @@
 // wants them a load touched 64 lines instead of 8 or 16, and the address units were what bound the kernel: 33 KB/us and compute unit),
 // reads them from there and multiplies, with no barrier.  The waves' partial sums are joined through LDS, in integers: the order does
 // not matter.  Decoding (a few tokens, kCols = 1) is bound by the weights' bytes; with more tokens the pieces grow, since a code of x
-// is read once per kCols pieces and one of w once per kBlocks, and the bound is the 60 KB/us that L2 gives a compute unit.  One token, 8-bit
+// is read once per kCols pieces and one of w once per kBlocks, and the bound is what a compute unit gets from L2, 87 KB/us of
+// direct loads alone, and the 3 to 4 us of start, first loads and joining.  One token, 8-bit
 // codes 4096 -> 4096: 4.6 us, 3.6 TB/s; 37 tokens, 4-bit weights 11008 -> 4096: 10.2 us, 2.2 TB/s of weights, each read twice.
 #pragma once
 

@@ -33,7 +33,7 @@ double pieces(const LinearArgs &A, int rows)
 }
 
 // What a kernel takes, in us.  The constants below are fits to a sweep of all kernels (1 .. 8192 tokens, (K, N) from (1024, 2048) to
-// (11008, 4096), (8192, 8192) and (4096, 32000), codes of 8, 4 and 2 bits, digits): what they choose is within 2.5 % of the best of the
+// (11008, 4096), (8192, 8192) and (4096, 32000), codes of 8, 4 and 2 bits, digits): what they choose is within 2 % of the best of the
 // sweep's kernels on average.  Measured, 8-bit codes 4096 -> 4096, us:
 //   tokens          1    16    32    64   128   256   512  1024  2048  4096  8192
 //   1x1           5.9   6.5   8.5  12.6  20.5  35.7  67.9   115
@@ -52,11 +52,12 @@ double weights_us(const LinearArgs &A, int wbits)
     return used * A.n * A.k * wbits / 8.0 / 4.4e6;
 }
 
-// A compute unit reads 50 KB of codes a us, and every workgroup has a prologue and the joining of its sums.
+// A compute unit reads 50 KB of codes a us, and every workgroup has a prologue and the joining of its sums.  Unpacking a weight, which every
+// workgroup does for itself, counts as another 0.8 (4 bits) or 2.4 bits of it (2 bits: without that 16 x 64 looked 20 % too good).
 double rows_us(const LinearArgs &A, int xbits, int wbits, int planes, int blocks, int cols)
 {
     const double rounds = pieces(A, 16 * blocks) * std::ceil(A.n / (16.0 * cols)) / kCUs;
-    const double kb = (16.0 * blocks * planes * xbits + 16.0 * cols * wbits) / 8.0 * A.k / 1000.0;
+    const double kb = (16.0 * blocks * planes * xbits + 16.0 * cols * (wbits == 8 ? 8.0 : wbits == 4 ? 4.8 : 4.4)) / 8.0 * A.k / 1000.0;
     const double codes = (rounds > 1.0 ? rounds : 1.0) * ((blocks * planes * cols >= 8 ? 2.1 : 1.1) + kb / 50.0);
     const double weights = weights_us(A, wbits);
     return 1.55 + (codes > weights ? codes : weights);

@@ -260,10 +260,11 @@ bq_status bq_linear_fwd(const void *x, const void *xscale, const void *w, const 
                         const bq_linear *desc, void *stream);
 
 /* The gradient with respect to the dequantised rows:  dx[t][k] = sum_o dy[t][o] wscale[o] w[o][k]   (the weights are codes and
- * stay as they are; with a straight-through round dx is the gradient of the rows that were quantised).  dy * wscale is taken
- * as a fixed-point number relative to the row's largest |dy * wscale|, of 16 bits for 16-bit rows and of 24 for float32: it is
- * off by at most 2^-15.9 or 2^-21.6 of that largest one, and the sums are exact.  Rows whose entries are all below
- * 2^-120 give 0; a row with an infinity or a NaN in dy * wscale gives NaN throughout.
+ * stay as they are; with a straight-through round dx is the gradient of the rows that were quantised).  dy * wscale is formed
+ * in float32 and enters the products with 22 of its bits for 16-bit rows (off by at most 2^-22 of itself) and with all of them
+ * for float32, whatever the row's other entries are; what lies below 2^-50 of the row's largest |dy * wscale| is lost.  Products
+ * are exact and sums float32, in an order that the descriptor fixes.  A row with an infinity or a NaN in dy * wscale gives NaN
+ * throughout.
  *   dy: [rows][ld_y], dx: [rows][ld_x], both of dtype; workspace: at least the queried size, 256-byte aligned, its contents
  *   on entry are ignored; calls that may run at once need one each.  dx must not overlap the inputs. */
 size_t bq_linear_bwd_workspace_bytes(const bq_linear *desc); /* 0 if the descriptor is invalid */

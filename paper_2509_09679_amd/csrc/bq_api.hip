@@ -493,7 +493,7 @@ static bq_status linear_fwd(bool grouped, const void *x, const void *xscale, con
     A.xs_f16 = A.ws_f16 = d->scale_dtype == BQ_F16;
     A.dtype = d->dtype;
     A.factor = 1.0f;
-    hipError_t e = bq::launch_linear(A, d->xbits, d->wbits, 1, (hipStream_t)stream);
+    hipError_t e = bq::launch_linear(A, d->xbits, d->wbits, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, who);
     return ok();
 }

@@ -260,7 +260,7 @@ hipError_t launch_row_quant(const void *x, int64_t rows, int cols, int64_t ld_x,
 // products of codes: bq_linear.h; their gradient: bq_linear_bwd.hip
 struct LinearArgs;
 struct LinearBwdLayout {
-    size_t factor, planes, weights, total;  // offsets into the workspace
+    size_t exponent, planes, weights, total;  // offsets into the workspace
 };
 LinearBwdLayout linear_bwd_layout(int64_t rows, int n, int k, int experts, int dtype);
 hipError_t launch_linear_bwd(const void *dy, int64_t ld_dy, const void *w, int wbits, int64_t ldw, const void *ws, int ws_f16,

@@ -6,9 +6,8 @@
 // as |x w| <= 2^14 and k < 2^17.  Packed codes are not sign-extended: a field is moved to the top of a byte, which makes it 16
 // (4 bits) or 64 (2 bits) times its value, and the epilogue's factor takes that out again (exact, a power of two).
 //
-// The gradient of the rows, dx[t, k] = sum_o dy[t, o] ws[o] w[o, k], is the same product: dy ws is written as a fixed-point
-// number relative to the row's largest entry, in `planes` base-256 digits of 8 bits, plane 0 the highest; a tile takes the
-// product of every plane and the epilogue joins them.
+// The gradient of the rows, dx[t, k] = sum_o dy[t, o] ws[o] w[o, k], is a product of the same form: dy ws is written as a sum of two or
+// three binary16 numbers, `terms` planes, and multiplied with the codes as binary16 numbers (exact) on v_mfma_f32_16x16x32_f16.
 //
 // The matrix instruction's first operand is the weights: a lane then holds consecutive channels of one token.
 #pragma once
@@ -22,7 +21,7 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 
 struct LinearArgs {
     const uint8_t *x, *w;
-    const void *xs, *ws, *bias;  // ws may be NULL (1), bias may be NULL (0)
+    const void *xs, *ws, *bias;  // xs: of a gradient the rows' exponents (int32), and no ws; bias may be NULL (0)
     void *y;
     const int32_t *offsets;  // [experts + 1], NULL: one expert that has all rows
     int64_t rows, ldx, ldw, ldy;  // ldx, ldw in bytes, ldy in elements
@@ -148,18 +147,20 @@ __device__ __forceinline__ void store_row_value(void *p, int64_t at, int dtype, 
 hipError_t launch_linear_any(const LinearArgs &A, int xbits, int wbits, hipStream_t stream);  // bq_linear_any.hip
 int64_t linear_any_blocks(const LinearArgs &A);
 // few rows: bq_linear_rows.h; blocks x cols: 16-token blocks and 16-channel columns of a workgroup
-hipError_t launch_linear_rows8(const LinearArgs &A, int wbits, int planes, int blocks, int cols, hipStream_t stream);
+hipError_t launch_linear_rows8(const LinearArgs &A, int wbits, int blocks, int cols, hipStream_t stream);
 hipError_t launch_linear_rows4(const LinearArgs &A, int wbits, int blocks, int cols, hipStream_t stream);
+hipError_t launch_linear_rows_terms(const LinearArgs &A, int terms, int blocks, int cols, hipStream_t stream);
 // many: bq_linear_tile.h
 enum LinearTile { kTileLarge, kTileTall, kTileMiddle, kTileSmall, kTileDeep };
 hipError_t launch_linear_tile8(const LinearArgs &A, int wbits, LinearTile tile, hipStream_t stream);
 hipError_t launch_linear_tile4(const LinearArgs &A, int wbits, LinearTile tile, hipStream_t stream);
-hipError_t launch_linear_tile_digits(const LinearArgs &A, int planes, LinearTile tile, hipStream_t stream);
-hipError_t launch_linear_tile_across(const LinearArgs &A, int wbits, int planes, LinearTile tile, hipStream_t stream);
-// picks the kernel; planes: 1 for codes, 2 or 3 for a gradient's digits (bq_linear.hip)
-hipError_t launch_linear(const LinearArgs &A, int xbits, int wbits, int planes, hipStream_t stream);
+hipError_t launch_linear_tile_terms(const LinearArgs &A, int terms, LinearTile tile, hipStream_t stream);
+hipError_t launch_linear_tile_across(const LinearArgs &A, int wbits, int terms, LinearTile tile, hipStream_t stream);
+// these pick the kernel (bq_linear.hip); a gradient has two or three terms
+hipError_t launch_linear(const LinearArgs &A, int xbits, int wbits, hipStream_t stream);
+hipError_t launch_linear_terms(const LinearArgs &A, int terms, hipStream_t stream);
 // the gradient's product with the weights as the layer has them, [summed index][channel]; is it quicker than transposing them first?
-bool linear_across_is_quicker(const LinearArgs &across, const LinearArgs &turned, int wbits, int planes);
-hipError_t launch_linear_across(const LinearArgs &A, int wbits, int planes, hipStream_t stream);
+bool linear_across_is_quicker(const LinearArgs &across, const LinearArgs &turned, int wbits, int terms);
+hipError_t launch_linear_across(const LinearArgs &A, int wbits, int terms, hipStream_t stream);
 
 }  // namespace bq

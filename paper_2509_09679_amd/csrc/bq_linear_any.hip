@@ -1,6 +1,6 @@
 // The product for any width, stride and alignment: a workgroup of four waves takes 64 tokens x 64 channels, its threads fetch the
 // codes one by one and lay them out as bytes in LDS.  Bound by those loads; the shapes of real layers go to the other kernels, and so do
-// all digits of gradients, whose rows are padded.
+// all gradients, whose rows are padded.
 #include "bq_linear.h"
 
 namespace bq {

@@ -1,12 +1,15 @@
-// What the gradient of a quantised product needs in front of the product itself: dy times the weights' scales as digits, and, where the
-// product does not read them as they lie, the weights' codes transposed, both with the summed index (the layer's outputs) contiguous and
-// padded with zeros.
+// What the gradient of a quantised product needs in front of the product itself: dy times the weights' scales as sums of binary16 numbers,
+// and, where the product does not read them as they lie, the weights' codes transposed, both with the summed index (the layer's outputs)
+// contiguous and padded with zeros.
 //
-// Digits.  v = dy ws is written as  v = f (256 d1 + d0)  (16-bit rows) or  f (65536 d2 + 256 d1 + d0)  (float32 rows), digits in
-// [-128, 127], f = max |v| / m with m = 32639 or 8355711, the largest number whose digits fit.  That rounds every term of the sum to
-// half of f: 2^-16 or 2^-24 of the row's largest term, against the 2^-9 or 2^-12 of the term itself that a product in the row's type
-// would leave.  Digits cost the matrix cores less than they look: two products of 8 bits take the time of one of 16 bits.  A row
-// with an infinity or NaN gets f = NaN: its gradient is NaN throughout.
+// Terms.  v = dy ws, a float32 number, times the power of two that brings the row's largest into [2^14, 2^15), is written as
+// h + 2^-11 (m + l), each the binary16 number nearest to what those before it leave: 22 bits of v with h and m (16-bit rows), 33 with
+// all three (float32 rows, so none of v's 24 is lost), whatever the row's other entries are.  What binary16's smallest number cuts off is
+// 2^-50 of the row's largest.  (Fixed-point digits relative to the row's largest entry, multiplied in integers, are half the
+// matrix cores' work, but lose the small entries of a row: of a softmax's gradient most of the sum.)  Two terms and not three for 16-bit
+// rows: the rounding of the result is 2^-12 or 2^-9, and three take half as long again.  The sums are float32, of the products with h and
+// of the others apart, so that only the former's roundings, one per 32 products, count; products of binary16 numbers are exact.  A row with
+// an infinity or a NaN has NaN in m: its gradient is NaN throughout.
 #include <type_traits>
 
 #include "bq_linear_codes.h"
@@ -16,14 +19,14 @@ namespace bq {
 
 namespace {
 
-struct DigitArgs {
+struct TermArgs {
     const void *dy, *ws;
-    int8_t *planes;   // [kPlanes][rows][np]
-    float *factor;    // [rows]
+    _Float16 *planes;  // [kTerms][rows][np]
+    int32_t *exponent; // [rows]: the terms are 2^-exponent times v
     const int32_t *offsets;
     int64_t rows, ld_dy;
     int n, np, experts, ws_f16;
-    int odd_last;  // eight digits lie as 0, 2, 4, 6, 1, 3, 5, 7: how packed codes come out of a word with the fewest steps
+    int spread;  // eight terms lie as 0, 4, 1, 5, 2, 6, 3, 7: how packed codes come out of a word with the fewest steps
 };
 
 // over a wave, or a workgroup of four
@@ -60,66 +63,51 @@ __device__ __forceinline__ int expert_of(const int32_t *offsets, int experts, in
     return -1;
 }
 
-// the factor of a row and what its entries are multiplied with, from the bit pattern of its largest magnitude
-struct RowFactor {
-    float lift, inv, factor;
-};
-
-template <int kPlanes>
-__device__ __forceinline__ RowFactor row_factor(uint32_t amax_bits)
+// what a row's entries are divided by, as a power of two, from the bit pattern of its largest magnitude
+__device__ __forceinline__ int row_exponent(uint32_t amax_bits)
 {
-    constexpr float kMost = kPlanes == 3 ? 8355711.0f : 32639.0f;
-    const bool finite = amax_bits < 0x7F800000u;
     const float amax = __uint_as_float(amax_bits);
-    // rows of tiny entries are lifted first: m / amax and amax / m have to be float32 numbers with all their digits; the factor's sign says so
-    RowFactor f;
-    f.lift = amax < 0x1p-60f ? 0x1p60f : 1.0f;
-    const float top = amax * f.lift;
-    const bool some = finite && top >= 0x1p-60f;  // (below 2^-120 the row counts as 0)
-    f.inv = some ? kMost / top : 0.0f;
-    f.factor = !finite ? __uint_as_float(0x7FC00000u) : some ? (f.lift != 1.0f ? -top : top) / kMost : 0.0f;
-    return f;
+    // (v_frexp_exp gives 0 for 0, infinities and NaN)
+    return amax_bits == 0 ? 0 : __builtin_amdgcn_frexp_expf(amax) - 15;
 }
 
-// The digits of 8 entries, packed by plane.  With u = rint(v inv) + 128 (+ 128 * 256), the digits are u's bytes, all but the highest less
-// 128; for two digits one addition to 1.5 * 2^23 both rounds and leaves u in the low bytes (|v inv| stays below m + 1/2).  The digits of
-// rows without a finite largest entry do not matter, those of a row that counts as 0 are 0.
-template <int kPlanes>
-__device__ __forceinline__ void digits8(float (&v)[8], const RowFactor &f, int odd_last, uint2 (&d)[kPlanes])
+// The terms of 8 entries, by plane.
+template <int kTerms>
+__device__ __forceinline__ void terms8(const float (&v)[8], int exponent, int spread, uint4 (&t)[kTerms])
 {
-    constexpr float kMost = 8355711.0f;
-    uint32_t u[8], w[kPlanes][2];
-    if (f.lift != 1.0f) {
+    float left[8];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) v[r] *= f.lift;
+    for (int r = 0; r < 8; ++r) {
+        const int from = r == 0 || r == 7 ? r : r % 2 ? (r + 7) / 2 : r / 2;  // 0, 4, 1, 5, 2, 6, 3, 7
+        left[r] = ldexpf(spread ? v[from] : v[r], -exponent);
     }
 #pragma unroll
-    for (int r = 0; r < 8; ++r)
-        u[r] = kPlanes == 2 ? __float_as_uint(__builtin_fmaf(v[r], f.inv, 0x1.8p23f + 128.0f))
-                            : (uint32_t)((int)__builtin_amdgcn_fmed3f(rintf(v[r] * f.inv), -kMost, kMost) + 0x8080);
+    for (int p = 0; p < kTerms; ++p) {
+        uint32_t w[4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint32_t *q = u + 4 * h;
-        const uint32_t a = __builtin_amdgcn_perm(q[1], q[0], 0x05010400u), b = __builtin_amdgcn_perm(q[3], q[2], 0x05010400u);
-        const uint32_t second = __builtin_amdgcn_perm(b, a, 0x07060302u);
-        w[kPlanes - 1][h] = __builtin_amdgcn_perm(b, a, 0x05040100u) ^ 0x80808080u;
-        w[kPlanes - 2][h] = kPlanes == 2 ? second : second ^ 0x80808080u;
-        if (kPlanes == 3)
-            w[0][h] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[3], q[2], 0x0C0C0602u), __builtin_amdgcn_perm(q[1], q[0], 0x0C0C0602u),
-                                            0x05040100u);
+        for (int j = 0; j < 4; ++j) {
+            w[j] = f32x2_to_f16x2_bits(left[2 * j], left[2 * j + 1]);
+            const f16x2 h = __builtin_bit_cast(f16x2, w[j]);
+#pragma unroll
+            for (int r = 0; r < 2; ++r) left[2 * j + r] = (left[2 * j + r] - (float)h[r]) * (p == 0 ? kLowerTerms : 1.0f);
+        }
+        t[p] = make_uint4(w[0], w[1], w[2], w[3]);
     }
+}
+
+template <int kTerms>
+__device__ __forceinline__ void store_terms(const TermArgs &A, int64_t row, int c, const uint4 (&t)[kTerms])
+{
 #pragma unroll
-    for (int p = 0; p < kPlanes; ++p)
-        d[p] = odd_last ? make_uint2(__builtin_amdgcn_perm(w[p][1], w[p][0], 0x06040200u), __builtin_amdgcn_perm(w[p][1], w[p][0], 0x07050301u))
-                        : make_uint2(w[p][0], w[p][1]);
+    for (int p = 0; p < kTerms; ++p) *(uint4 *)(A.planes + ((int64_t)p * A.rows + row) * A.np + c) = t[p];
 }
 
 // kThreads, a wave or the workgroup, take rows_each neighbouring rows, which mostly belong to one expert, and keep that expert's scales and
 // a row's products in registers; kPasses pieces per thread.  kWhole: the rows' pieces are whole.  One read of dy and one write of the
-// digits: bound by HBM, and for a few thousand rows by the turns to memory that a row takes one after another.  4096 rows of 1408 of 8
-// experts, bf16: 8.8 us with workgroups, 7.7 us with waves (3.0 TB/s); 2048 rows of 4096: 8.1 us (4.1 TB/s).
-template <typename T, int kPlanes, int kThreads, int kPasses, bool kWhole>
-__device__ __forceinline__ void digit_rows(const DigitArgs &A, int64_t block, int rows_each)
+// terms: bound by HBM, and for a few thousand rows by the turns to memory that a row takes one after another.  bf16, 4096 rows of 1408
+// of 8 experts: 8.4 us (4.1 TB/s); 2048 rows of 4096: 9 us (5.6 TB/s).
+template <typename T, int kTerms, int kThreads, int kPasses, bool kWhole>
+__device__ __forceinline__ void term_rows(const TermArgs &A, int64_t block, int rows_each)
 {
     const int thread = threadIdx.x % kThreads;
     const int64_t first = (block * (256 / kThreads) + threadIdx.x / kThreads) * rows_each;
@@ -162,23 +150,22 @@ __device__ __forceinline__ void digit_rows(const DigitArgs &A, int64_t block, in
                 m = m > b ? m : b;
             }
         }
-        const RowFactor f = row_factor<kPlanes>(max_over<kThreads>(m));
-        if (thread == 0) A.factor[row] = f.factor;
+        const int exponent = row_exponent(max_over<kThreads>(m));
+        if (thread == 0) A.exponent[row] = exponent;
 #pragma unroll
         for (int p = 0; p < kPasses; ++p) {
             const int c = (p * kThreads + thread) * 8;
             if (c >= A.np) continue;
-            uint2 d[kPlanes];
-            digits8<kPlanes>(v[p], f, A.odd_last, d);
-#pragma unroll
-            for (int q = 0; q < kPlanes; ++q) *(uint2 *)(A.planes + ((int64_t)q * A.rows + row) * A.np + c) = d[q];
+            uint4 t[kTerms];
+            terms8<kTerms>(v[p], exponent, A.spread, t);
+            store_terms<kTerms>(A, row, c, t);
         }
     }
 }
 
 // Wider rows; the second look at a row comes from the caches.
-template <typename T, int kPlanes>
-__device__ __forceinline__ void digit_rows_wide(const DigitArgs &A, int64_t block, int rows_each)
+template <typename T, int kTerms>
+__device__ __forceinline__ void term_rows_wide(const TermArgs &A, int64_t block, int rows_each)
 {
     const int64_t end = (block + 1) * rows_each < A.rows ? (block + 1) * rows_each : A.rows;
     for (int64_t row = block * rows_each; row < end; ++row) {
@@ -192,16 +179,15 @@ __device__ __forceinline__ void digit_rows_wide(const DigitArgs &A, int64_t bloc
             const uint32_t b = __float_as_uint(entry(c)) & 0x7FFFFFFFu;
             m = m > b ? m : b;
         }
-        const RowFactor f = row_factor<kPlanes>(max_over<256>(m));
-        if (threadIdx.x == 0) A.factor[row] = f.factor;
+        const int exponent = row_exponent(max_over<256>(m));
+        if (threadIdx.x == 0) A.exponent[row] = exponent;
         for (int c = threadIdx.x * 8; c < A.np; c += 2048) {
             float v[8];
 #pragma unroll
             for (int r = 0; r < 8; ++r) v[r] = entry(c + r);
-            uint2 d[kPlanes];
-            digits8<kPlanes>(v, f, A.odd_last, d);
-#pragma unroll
-            for (int q = 0; q < kPlanes; ++q) *(uint2 *)(A.planes + ((int64_t)q * A.rows + row) * A.np + c) = d[q];
+            uint4 t[kTerms];
+            terms8<kTerms>(v, exponent, A.spread, t);
+            store_terms<kTerms>(A, row, c, t);
         }
     }
 }
@@ -221,7 +207,7 @@ constexpr int kTr = 128;
 // 128 outputs x 128 inputs per workgroup, workgroup `block` of all.  A thread reads 16 codes of four neighbouring outputs, turns them in
 // registers, 4 x 4 bytes at a time, and stores words of four outputs to LDS, from where the result's rows leave in whole lines.  Codes of 4
 // and 2 bits come out as bytes with the code at the top, 16 or 64 times its value.  One read of w, one write: bound by HBM (4096 x 4096 bytes
-// with the digits of 2048 bf16 rows: 13.5 us, 5.0 TB/s).
+// beside the terms of 2048 bf16 rows: 13.5 us, 5.0 TB/s).
 template <int kBits>
 __device__ __forceinline__ void transpose_tile(const TransposeArgs &A, uint32_t block)
 {
@@ -270,24 +256,24 @@ __device__ __forceinline__ void transpose_tile(const TransposeArgs &A, uint32_t 
     }
 }
 
-// Both in one launch: neither needs the other.  The first digit_blocks workgroups write digits (kPasses 0: of the widest rows), the others
+// Both in one launch: neither needs the other.  The first term_blocks workgroups write terms (kPasses 0: of the widest rows), the others
 // transpose (kBits 0: there are none).
-template <typename T, int kPlanes, int kThreads, int kPasses, bool kWhole, int kBits>
-__global__ __launch_bounds__(256) void linear_prepare_kernel(DigitArgs D, int rows_each, uint32_t digit_blocks, TransposeArgs R)
+template <typename T, int kTerms, int kThreads, int kPasses, bool kWhole, int kBits>
+__global__ __launch_bounds__(256) void linear_prepare_kernel(TermArgs D, int rows_each, uint32_t term_blocks, TransposeArgs R)
 {
     if constexpr (kBits != 0) {
-        if (blockIdx.x >= digit_blocks) {
-            transpose_tile<kBits>(R, blockIdx.x - digit_blocks);
+        if (blockIdx.x >= term_blocks) {
+            transpose_tile<kBits>(R, blockIdx.x - term_blocks);
             return;
         }
     }
     if constexpr (kPasses == 0)
-        digit_rows_wide<T, kPlanes>(D, blockIdx.x, rows_each);
+        term_rows_wide<T, kTerms>(D, blockIdx.x, rows_each);
     else
-        digit_rows<T, kPlanes, kThreads, kPasses, kWhole>(D, blockIdx.x, rows_each);
+        term_rows<T, kTerms, kThreads, kPasses, kWhole>(D, blockIdx.x, rows_each);
 }
 
-// The same for any width and alignment, 64 x 64 codes one by one.
+// The transposition for any width and alignment, 64 x 64 codes one by one.
 __global__ __launch_bounds__(256) void linear_transpose_any_kernel(TransposeArgs A, int bits)
 {
     __shared__ __align__(16) uint8_t s[64][64 + 4];
@@ -308,26 +294,26 @@ __global__ __launch_bounds__(256) void linear_transpose_any_kernel(TransposeArgs
     for (int j = 0; j < 16; ++j) A.out[((int64_t)expert * A.k + k) * A.np + o0 + part + j] = (int8_t)s[part + j][row];
 }
 
-int padded(int n) { return (n + 127) / 128 * 128; }
+int padded(int n) { return (n + 127) / 128 * 128; }  // rows' strides; the products sum over whole stages of 64
 
-template <typename T, int kPlanes, int kBits>
-hipError_t launch_prepare(const DigitArgs &D, const TransposeArgs &R, uint32_t transpose_blocks, hipStream_t stream)
+template <typename T, int kTerms, int kBits>
+hipError_t launch_prepare(const TermArgs &D, const TransposeArgs &R, uint32_t transpose_blocks, hipStream_t stream)
 {
     auto launch = [&](auto THREADS, auto PASSES) {
         constexpr int threads = decltype(THREADS)::value, passes = decltype(PASSES)::value, at_once = 256 / threads;
         // beyond 16384 waves they take several rows each
         const int rows_each = (int)((D.rows + 4096 * at_once - 1) / (4096 * at_once));
         const int64_t per_block = (int64_t)rows_each * at_once;
-        const uint32_t digit_blocks = (uint32_t)((D.rows + per_block - 1) / per_block);
-        const dim3 grid(digit_blocks + transpose_blocks);
+        const uint32_t term_blocks = (uint32_t)((D.rows + per_block - 1) / per_block);
+        const dim3 grid(term_blocks + transpose_blocks);
         if constexpr (passes != 0) {
             if (D.n % 8 == 0) {
-                hipLaunchKernelGGL((linear_prepare_kernel<T, kPlanes, threads, passes, true, kBits>), grid, dim3(256), 0, stream, D, rows_each,
-                                   digit_blocks, R);
+                hipLaunchKernelGGL((linear_prepare_kernel<T, kTerms, threads, passes, true, kBits>), grid, dim3(256), 0, stream, D, rows_each,
+                                   term_blocks, R);
                 return hipGetLastError();
             }
         }
-        hipLaunchKernelGGL((linear_prepare_kernel<T, kPlanes, threads, passes, false, kBits>), grid, dim3(256), 0, stream, D, rows_each, digit_blocks,
+        hipLaunchKernelGGL((linear_prepare_kernel<T, kTerms, threads, passes, false, kBits>), grid, dim3(256), 0, stream, D, rows_each, term_blocks,
                            R);
         return hipGetLastError();
     };
@@ -346,18 +332,18 @@ hipError_t launch_prepare(const DigitArgs &D, const TransposeArgs &R, uint32_t t
     return launch(Workgroup{}, std::integral_constant<int, 8>{});
 }
 
-// digits, and unless bits is 0 the weights
-template <typename T, int kPlanes>
-hipError_t prepare(const DigitArgs &D, const TransposeArgs &R, int bits, hipStream_t stream)
+// terms, and unless bits is 0 the weights
+template <typename T, int kTerms>
+hipError_t prepare(const TermArgs &D, const TransposeArgs &R, int bits, hipStream_t stream)
 {
-    if (bits == 0) return launch_prepare<T, kPlanes, 0>(D, R, 0, stream);
+    if (bits == 0) return launch_prepare<T, kTerms, 0>(D, R, 0, stream);
     const int64_t tiles = (int64_t)((R.k + kTr - 1) / kTr) * (R.np / kTr) * D.experts;
     if (R.k % 16 == 0 && (uintptr_t)R.w % (2 * bits) == 0 && R.ldw % (2 * bits) == 0 && tiles < (int64_t)1 << 23) {
-        if (bits == 8) return launch_prepare<T, kPlanes, 8>(D, R, (uint32_t)tiles, stream);
-        if (bits == 4) return launch_prepare<T, kPlanes, 4>(D, R, (uint32_t)tiles, stream);
-        return launch_prepare<T, kPlanes, 2>(D, R, (uint32_t)tiles, stream);
+        if (bits == 8) return launch_prepare<T, kTerms, 8>(D, R, (uint32_t)tiles, stream);
+        if (bits == 4) return launch_prepare<T, kTerms, 4>(D, R, (uint32_t)tiles, stream);
+        return launch_prepare<T, kTerms, 2>(D, R, (uint32_t)tiles, stream);
     }
-    const hipError_t e = launch_prepare<T, kPlanes, 0>(D, R, 0, stream);
+    const hipError_t e = launch_prepare<T, kTerms, 0>(D, R, 0, stream);
     if (e != hipSuccess) return e;
     const dim3 grid((unsigned)((R.k + 63) / 64), (unsigned)(R.np / 64), (unsigned)D.experts);
     hipLaunchKernelGGL(linear_transpose_any_kernel, grid, dim3(256), 0, stream, R, bits);
@@ -366,15 +352,15 @@ hipError_t prepare(const DigitArgs &D, const TransposeArgs &R, int bits, hipStre
 
 }  // namespace
 
-int linear_planes(int dtype) { return dtype == BQ_F32 ? 3 : 2; }
+int linear_terms(int dtype) { return dtype == BQ_F32 ? 3 : 2; }
 
 LinearBwdLayout linear_bwd_layout(int64_t rows, int n, int k, int experts, int dtype)
 {
     LinearBwdLayout L;
     const size_t np = (size_t)padded(n);
-    L.factor = 0;
-    L.planes = align256((size_t)rows * sizeof(float));
-    L.weights = L.planes + align256((size_t)linear_planes(dtype) * (size_t)rows * np);
+    L.exponent = 0;
+    L.planes = align256((size_t)rows * sizeof(int32_t));
+    L.weights = L.planes + align256((size_t)linear_terms(dtype) * (size_t)rows * np * sizeof(_Float16));
     L.total = L.weights + align256((size_t)experts * (size_t)k * np);
     return L;
 }
@@ -385,12 +371,12 @@ hipError_t launch_linear_bwd(const void *dy, int64_t ld_dy, const void *w, int w
 {
     const LinearBwdLayout L = linear_bwd_layout(rows, n, k, experts, dtype);
     char *base = (char *)workspace;
-    const int np = padded(n), planes = linear_planes(dtype);
-    DigitArgs D{};
+    const int np = padded(n), terms = linear_terms(dtype);
+    TermArgs D{};
     D.dy = dy;
     D.ws = ws;
-    D.planes = (int8_t *)(base + L.planes);
-    D.factor = (float *)(base + L.factor);
+    D.planes = (_Float16 *)(base + L.planes);
+    D.exponent = (int32_t *)(base + L.exponent);
     D.offsets = offsets;
     D.rows = rows;
     D.ld_dy = ld_dy;
@@ -410,15 +396,16 @@ hipError_t launch_linear_bwd(const void *dy, int64_t ld_dy, const void *w, int w
     LinearArgs A{};
     A.x = (const uint8_t *)(base + L.planes);
     A.w = (const uint8_t *)(base + L.weights);
-    A.xs = base + L.factor;
+    A.xs = base + L.exponent;
     A.y = dx;
     A.offsets = offsets;
     A.rows = rows;
-    A.ldx = A.ldw = np;
+    A.ldx = np * (int64_t)sizeof(_Float16);
+    A.ldw = np;
     A.ldy = ld_dx;
     A.w_step = (int64_t)k * np;
-    A.plane_step = rows * np;
-    A.k = np;
+    A.plane_step = rows * A.ldx;
+    A.k = (n + 63) / 64 * 64;
     A.n = k;
     A.experts = experts;
     A.dtype = dtype;
@@ -428,16 +415,16 @@ hipError_t launch_linear_bwd(const void *dy, int64_t ld_dy, const void *w, int w
     across.ldw = ldw;
     across.w_step = R.w_step;
     across.w_rows = n;
-    const bool as_they_are = linear_across_is_quicker(across, A, wbits, planes);
+    const bool as_they_are = linear_across_is_quicker(across, A, wbits, terms);
     const int turn = as_they_are ? 0 : wbits;
-    D.odd_last = as_they_are && wbits < 8;
+    D.spread = as_they_are && wbits < 8;
     const hipError_t e = dtype == BQ_F32   ? prepare<float, 3>(D, R, turn, stream)
                          : dtype == BQ_F16 ? prepare<__half, 2>(D, R, turn, stream)
                                            : prepare<bf16_t, 2>(D, R, turn, stream);
     if (e != hipSuccess) return e;
-    if (as_they_are) return launch_linear_across(across, wbits, planes, stream);
+    if (as_they_are) return launch_linear_across(across, wbits, terms, stream);
     A.factor /= (float)(1 << (8 - wbits));
-    return launch_linear(A, 8, 8, planes, stream);
+    return launch_linear_terms(A, terms, stream);
 }
 
 }  // namespace bq

@@ -74,35 +74,76 @@ __device__ __forceinline__ int lds_turn(int row)
     return kRowBytes == 64 ? (row >> 2) & 2 : ((row >> 1) & 1) | (kPieces == 2 ? (row >> 1) & 4 : (row >> 2) & 2);
 }
 
-// what the epilogues have in common: the value of one result from its sums (one per plane)
-template <int kPlanes>
-__device__ __forceinline__ float joined(const int (&sum)[kPlanes])
+// ---- codes of weights as binary16 numbers, for a gradient.  A field in the low bits of a binary16 number with the exponent of 1024 is 1024
+// plus its value; packed binary16 operations move that to the code itself, exactly.
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ uint32_t f16_pair(f16x2 v) { return __builtin_bit_cast(uint32_t, v); }
+
+// the fields of kBits at bit kAt of both halves of w, whose top bits are turned round, as codes
+template <int kBits, int kAt>
+__device__ __forceinline__ uint32_t half_fields(uint32_t w)
 {
-    if constexpr (kPlanes == 1) return (float)sum[0];
-    // (two digits serve 16-bit results: what float32 loses of the lower sum is 2^-17 of the digits' own rounding)
-    if constexpr (kPlanes == 2) return __builtin_fmaf((float)sum[0], 256.0f, (float)sum[1]);
-    if constexpr (kPlanes == 3) return (float)__builtin_fma((double)sum[0], 65536.0, __builtin_fma((double)sum[1], 256.0, (double)sum[2]));
+    constexpr uint32_t kMask = ((1u << kBits) - 1) << kAt;
+    constexpr float kStep = 1.0f / (1 << kAt), kOffset = -(1024.0f * kStep + (1 << (kBits - 1)));
+    const f16x2 v = __builtin_bit_cast(f16x2, (w & (kMask << 16 | kMask)) | 0x64006400u);
+    return f16_pair(__builtin_elementwise_fma(v, f16x2{(_Float16)kStep, (_Float16)kStep}, f16x2{(_Float16)kOffset, (_Float16)kOffset}));
 }
 
-// What a token's sums are multiplied with.  The fields' factor, a power of two, goes to the sum, where it is exact: a scale near float32's
-// smallest would lose digits to it.  A gradient's row factor is negative if the row was lifted by 2^60 (bq_linear_bwd.hip).
-struct TokenScale {
-    float fields, scale, lower;
+// 8 codes of 8 bits, in order
+__device__ __forceinline__ i32x4 half_codes8(uint32_t lo, uint32_t hi)
+{
+    i32x4 r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t w = __builtin_amdgcn_perm(0x64646464u, (j < 2 ? lo : hi) ^ 0x80808080u, j % 2 ? 0x04030402u : 0x04010400u);
+        r[j] = (int)f16_pair(__builtin_bit_cast(f16x2, w) - f16x2{(_Float16)1152.0f, (_Float16)1152.0f});
+    }
+    return r;
+}
+
+// 8 codes of 4 bits, as 0, 4, 1, 5, 2, 6, 3, 7
+__device__ __forceinline__ i32x4 half_codes4(uint32_t w)
+{
+    const uint32_t u = w ^ 0x88888888u, v = u >> 8;
+    return i32x4{(int)half_fields<4, 0>(u), (int)half_fields<4, 4>(u), (int)half_fields<4, 0>(v), (int)half_fields<4, 4>(v)};
+}
+
+// the same of the even channel (odd = 0) or the odd one of 8 fields of 4 bits that hold two codes of 2 bits each
+__device__ __forceinline__ i32x4 half_codes2(uint32_t w, int odd)
+{
+    const uint32_t u = w ^ 0xAAAAAAAAu, v = u >> 8;
+    if (odd) return i32x4{(int)half_fields<2, 2>(u), (int)half_fields<2, 6>(u), (int)half_fields<2, 2>(v), (int)half_fields<2, 6>(v)};
+    return i32x4{(int)half_fields<2, 0>(u), (int)half_fields<2, 4>(u), (int)half_fields<2, 0>(v), (int)half_fields<2, 4>(v)};
+}
+
+// ---- what products of codes (int32 sums) and gradients (binary16 terms, float32 sums) have in common
+
+template <bool kFloat>
+struct SumType {
+    typedef i32x4 type;
+};
+template <>
+struct SumType<true> {
+    typedef f32x4 type;
 };
 
-template <int kPlanes>
-__device__ __forceinline__ TokenScale token_scale(float scale, float fields)
+__device__ __forceinline__ i32x4 multiply(i32x4 w, i32x4 x, i32x4 sum) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, sum, 0, 0, 0); }
+__device__ __forceinline__ f32x4 multiply(i32x4 w, i32x4 x, f32x4 sum)
 {
-    if constexpr (kPlanes == 1) return TokenScale{fields, scale, 1.0f};
-    return TokenScale{fields, fabsf(scale), scale < 0.0f ? 0x1p-60f : 1.0f};
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, w), __builtin_bit_cast(f16x8, x), sum, 0, 0, 0);
 }
 
-template <int kPlanes>
-__device__ __forceinline__ float scaled(const int (&sum)[kPlanes], const TokenScale &s)
-{
-    const float v = joined<kPlanes>(sum) * s.fields * s.scale;
-    return kPlanes == 1 ? v : v * s.lower;
-}
+// The value of one result.  The fields' factor, a power of two, goes to the sum, where it is exact: a scale near float32's smallest would
+// lose digits to it.
+__device__ __forceinline__ float scaled(int sum, float fields, float xs, float ws) { return (float)sum * fields * xs * ws; }
+
+// a gradient's: the terms behind the first are kept 2^11 times their size (bq_linear_bwd.hip)
+constexpr float kLowerTerms = 0x1p11f;
+__device__ __forceinline__ float terms_sum(float first, float others) { return __builtin_fmaf(others, 1.0f / kLowerTerms, first); }
 
 // scales and bias of some channels or tokens: every type's loads in a branch of its own, so that they are in flight together
 template <int kCount>
@@ -114,21 +155,6 @@ __device__ __forceinline__ void load_scales(const void *p, int f16, const int64_
     } else {
 #pragma unroll
         for (int c = 0; c < kCount; ++c) s[c] = ((const float *)p)[at[c]];
-    }
-}
-template <int kCount>
-__device__ __forceinline__ void token_scales(const LinearArgs &A, const int64_t (&at)[kCount], float (&s)[kCount])
-{
-    load_scales(A.xs, A.xs_f16, at, s);
-}
-template <int kCount>
-__device__ __forceinline__ void channel_scales(const LinearArgs &A, const int64_t (&at)[kCount], float (&s)[kCount])
-{
-    if (A.ws) {
-        load_scales(A.ws, A.ws_f16, at, s);
-    } else {
-#pragma unroll
-        for (int c = 0; c < kCount; ++c) s[c] = 1.0f;
     }
 }
 template <int kCount>

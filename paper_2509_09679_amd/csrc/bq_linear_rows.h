@@ -2,8 +2,8 @@
 // step, so that the workgroup reads its channels' codes front to back, every code once, and every wave works for itself: it loads
 // the codes of its steps into a ring of its own in LDS (directly, 16 bytes per lane, whole lines: in the order the matrix instruction
 // wants them a load touched 64 lines instead of 8 or 16, and the address units were what bound the kernel: 33 KB/us and compute unit),
-// reads them from there and multiplies, with no barrier.  The waves' partial sums are joined through LDS, in integers: the order does
-// not matter.  Decoding (a few tokens, kCols = 1) is bound by the weights' bytes; with more tokens the pieces grow, since a code of x
+// reads them from there and multiplies, with no barrier.  The waves' partial sums are joined through LDS, integers in whatever order, a
+// gradient's float32 sums wave after wave.  Decoding (a few tokens, kCols = 1) is bound by the weights' bytes; with more tokens the pieces grow, since a code of x
 // is read once per kCols pieces and one of w once per kBlocks, and the bound is what a compute unit gets from L2, 87 KB/us of
 // direct loads alone, and the 3 to 4 us of start, first loads and joining.  One token, 8-bit
 // codes 4096 -> 4096: 4.6 us, 3.6 TB/s; 37 tokens, 4-bit weights 11008 -> 4096: 10.2 us, 2.2 TB/s of weights, each read twice.
@@ -14,34 +14,36 @@
 namespace bq {
 
 // kWide: all of a compute unit's LDS for one workgroup, else half of it.
-template <int kXBits, int kWBits, int kPlanes, int kBlocks, int kCols, bool kWide>
+template <int kXBits, int kWBits, int kTerms, int kBlocks, int kCols, bool kWide>
 struct RowsShape {
-    static constexpr int frags = kBlocks * kPlanes;
-    static constexpr int codes = kWBits == 2 ? 256 : 128;                       // of a step
+    static constexpr int frags = kBlocks * kTerms;
+    static constexpr int codes = kXBits == 16 ? 64 : kWBits == 2 ? 256 : 128;   // of a step
     static constexpr int x_row = codes * kXBits / 8, w_row = codes * kWBits / 8;  // bytes of a step's rows: 64, 128, 256
     static constexpr int x_bytes = frags * 16 * x_row, w_bytes = kCols * 16 * w_row, step = x_bytes + w_bytes;
     static constexpr int room = (kWide ? 160 : 80) * 1024;
     static constexpr int waves = 16 * step <= room ? 8 : 4;
     static constexpr int per_simd = kWide ? 2 : waves / 2;  // waves that have to fit (four alone would get registers they have no use for)
     static constexpr int fit = room / (waves * step), depth = fit < 4 ? fit : 4;
-    static constexpr int pairs = kBlocks * kCols, most = waves / kPlanes, chunk = pairs < most ? pairs : most;  // pieces joined at a time
-    static constexpr int joined = waves * chunk * kPlanes * 1024;
+    static constexpr int pairs = kBlocks * kCols, chunk = pairs < waves ? pairs : waves;  // pieces joined at a time
+    static constexpr int joined = waves * chunk * 1024;
     static constexpr int lds = waves * depth * step > joined ? waves * depth * step : joined;
     static constexpr bool exists = depth >= 2;  // one step is multiplied while another is loaded
 };
 
-template <int kXBits, int kWBits, int kPlanes, int kBlocks, int kCols, bool kWide>
-__global__ __launch_bounds__((64 * RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols, kWide>::waves),
-                             (RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols, kWide>::per_simd)) void linear_rows_kernel(LinearArgs A)
+template <int kXBits, int kWBits, int kTerms, int kBlocks, int kCols, bool kWide>
+__global__ __launch_bounds__((64 * RowsShape<kXBits, kWBits, kTerms, kBlocks, kCols, kWide>::waves),
+                             (RowsShape<kXBits, kWBits, kTerms, kBlocks, kCols, kWide>::per_simd)) void linear_rows_kernel(LinearArgs A)
 {
-    typedef RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols, kWide> S;
+    typedef RowsShape<kXBits, kWBits, kTerms, kBlocks, kCols, kWide> S;
     constexpr int kFrags = S::frags, kWaves = S::waves, kDepth = S::depth, kPairs = S::pairs, kChunk = S::chunk;
     constexpr int kXSub = S::x_row == 256 ? 2 : 1, kXLine = S::x_row / kXSub;  // rows of 256 bytes lie as two of 128
     constexpr int kXWords = S::x_row / 16, kWWords = S::w_row / 16;            // of a lane: a quarter of a row
     constexpr int kXLoads = S::x_bytes / 1024, kWLoads = S::w_bytes / 1024, kLoads = kXLoads + kWLoads;
-    constexpr bool kNatural = kXBits != kWBits;
+    constexpr bool kFloat = kXBits == 16, kNatural = kXBits != kWBits;
+    static_assert(kFloat == (kTerms > 1) && (!kFloat || kWBits == 8), "codes, or a gradient");
+    typedef typename SumType<kFloat>::type Sum;
     extern __shared__ __align__(16) uint8_t rows_lds[];
-    i32x4(*const s_part)[kChunk * kPlanes][64] = (i32x4(*)[kChunk * kPlanes][64])rows_lds;
+    Sum(*const s_part)[kChunk][64] = (Sum(*)[kChunk][64])rows_lds;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r16 = lane & 15, g = lane >> 4;
     const int o0 = blockIdx.x * 16 * kCols;
@@ -74,10 +76,10 @@ __global__ __launch_bounds__((64 * RowsShape<kXBits, kWBits, kPlanes, kBlocks, k
         for (int i = 0; i < kXLoads; ++i) {
             // x lies as [half of a row][plane and 16 tokens][token]
             const int line = i * (1024 / kXLine) + lane / (kXLine / 16), half = i * (1024 / kXLine) / (16 * kFrags);
-            const int frag = i * (1024 / kXLine) / 16 % kFrags, token = 16 * (frag / kPlanes) + line % 16;
+            const int frag = i * (1024 / kXLine) / 16 % kFrags, token = 16 * (frag / kTerms) + line % 16;
             const int last = (int)(row_b - row0 < pass ? row_b - row0 : pass) - 1;
             x_piece[i] = half * 8 + ((lane % (kXLine / 16)) ^ lds_turn<kXLine, kXWords / 4>(line & 15));
-            x_base[i] = A.x + (frag % kPlanes) * A.plane_step + row0 * A.ldx;
+            x_base[i] = A.x + (frag % kTerms) * A.plane_step + row0 * A.ldx;
             x_off[i] = (uint32_t)(token < last ? token : last) * (uint32_t)A.ldx;
         }
         auto load = [&](int i, int place) {  // the wave's i-th step
@@ -92,7 +94,8 @@ __global__ __launch_bounds__((64 * RowsShape<kXBits, kWBits, kPlanes, kBlocks, k
                 load_to_lds(ring0 + place * S::step + S::x_bytes + n * 1024,
                             w_off[n] + (last && w_tail && w_piece[n] >= w_tail ? 0 : w_piece[n]) * 16, w_base + (int64_t)s * S::w_row);
         };
-        i32x4 acc[kCols][kFrags] = {};
+        constexpr int kSums = kFloat ? 2 * kBlocks : kBlocks;  // (first terms, others)
+        Sum acc[kCols][kSums] = {};
         if (row0 != row_a + blockIdx.y * pass) __syncthreads();  // the pass before has read its sums
         for (int i = 0; i < kDepth && i < mine; ++i) load(i, i);
         for (int i = 0, place = 0; i < mine; ++i) {
@@ -130,15 +133,23 @@ __global__ __launch_bounds__((64 * RowsShape<kXBits, kWBits, kPlanes, kBlocks, k
                         if (g * (kXWords / 4) + j / 4 >= x_tail) xv[f][j] = 0;
             }
 #pragma unroll
-            for (int s = 0; s < S::codes / 64; ++s) {
+            for (int s = 0; s < S::codes / (kFloat ? 32 : 64); ++s) {
                 i32x4 a[kCols];
 #pragma unroll
-                for (int c = 0; c < kCols; ++c) a[c] = step_codes<kWBits, kNatural>(wv[c], s);
+                for (int c = 0; c < kCols; ++c) {
+                    if constexpr (kFloat)
+                        a[c] = half_codes8(wv[c][2 * s], wv[c][2 * s + 1]);
+                    else
+                        a[c] = step_codes<kWBits, kNatural>(wv[c], s);
+                }
 #pragma unroll
                 for (int f = 0; f < kFrags; ++f) {
-                    const i32x4 b = step_codes<kXBits, kNatural>(xv[f], s);
+                    const i32x4 b = step_codes<kFloat ? 8 : kXBits, kNatural>(xv[f], s);  // (terms lie as 16 bytes of a step, too)
 #pragma unroll
-                    for (int c = 0; c < kCols; ++c) acc[c][f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[c], b, acc[c][f], 0, 0, 0);
+                    for (int c = 0; c < kCols; ++c) {
+                        Sum &sum = acc[c][kFloat ? f / kTerms * 2 + (f % kTerms != 0) : f];
+                        sum = multiply(a[c], b, sum);
+                    }
                 }
             }
         }
@@ -146,56 +157,64 @@ __global__ __launch_bounds__((64 * RowsShape<kXBits, kWBits, kPlanes, kBlocks, k
         for (int first = 0; first < kPairs; first += kChunk) {
             __syncthreads();  // (the codes, or the sums before, have been read)
 #pragma unroll
-            for (int i = 0; i < kChunk; ++i)
+            for (int i = 0; i < kChunk; ++i) {
+                if (first + i >= kPairs) continue;
+                const Sum *const piece = acc[(first + i) / kBlocks];
+                const int b = (first + i) % kBlocks;
+                if constexpr (kFloat) {
+                    Sum v;
 #pragma unroll
-                for (int p = 0; p < kPlanes; ++p)
-                    if (first + i < kPairs) s_part[wave][i * kPlanes + p][lane] = acc[(first + i) / kBlocks][(first + i) % kBlocks * kPlanes + p];
+                    for (int r = 0; r < 4; ++r) v[r] = terms_sum(piece[2 * b][r], piece[2 * b + 1][r]);
+                    s_part[wave][i][lane] = v;
+                } else {
+                    s_part[wave][i][lane] = piece[b];
+                }
+            }
             __syncthreads();
             const int pair = first + wave, block = pair % kBlocks, col = pair / kBlocks;
             if (wave >= kChunk || pair >= kPairs) continue;
-            i32x4 sum[kPlanes];
+            Sum sum = s_part[0][wave][lane];
 #pragma unroll
-            for (int p = 0; p < kPlanes; ++p) {
-                sum[p] = s_part[0][wave * kPlanes + p][lane];
-#pragma unroll
-                for (int v = 1; v < kWaves; ++v) sum[p] += s_part[v][wave * kPlanes + p][lane];
-            }
+            for (int v = 1; v < kWaves; ++v) sum += s_part[v][wave][lane];
             const int64_t t = row0 + 16 * block + r16;
             const int o = o0 + 16 * col + 4 * g;
             if (t >= row_b || o >= A.n) continue;
-            const TokenScale xs = token_scale<kPlanes>(load_scale(A.xs, t, A.xs_f16), A.factor);
-            int64_t at[4];
+            float v[4];
+            if constexpr (kFloat) {
+                const int exponent = ((const int *)A.xs)[t];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) at[r] = (int64_t)expert * A.n + (o + r < A.n ? o + r : A.n - 1);
-            float ws[4], bias[4], v[4];
-            channel_scales(A, at, ws);
-            channel_bias(A, at, bias);
+                for (int r = 0; r < 4; ++r) v[r] = ldexpf(sum[r] * A.factor, exponent);
+            } else {
+                const float xs = load_scale(A.xs, t, A.xs_f16);
+                int64_t at[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                int part[kPlanes];
+                for (int r = 0; r < 4; ++r) at[r] = (int64_t)expert * A.n + (o + r < A.n ? o + r : A.n - 1);
+                float ws[4], bias[4];
+                load_scales(A.ws, A.ws_f16, at, ws);
+                channel_bias(A, at, bias);
 #pragma unroll
-                for (int p = 0; p < kPlanes; ++p) part[p] = sum[p][r];
-                v[r] = scaled<kPlanes>(part, xs);
-                if (A.ws) v[r] *= ws[r];
-                if (A.bias) v[r] += bias[r];
+                for (int r = 0; r < 4; ++r) {
+                    v[r] = scaled(sum[r], A.factor, xs, ws[r]);
+                    if (A.bias) v[r] += bias[r];
+                }
             }
             store_results<4>(A, t * A.ldy + o, v, A.n - o);
         }
     }
 }
 
-template <int kXBits, int kWBits, int kPlanes, int kBlocks, int kCols, bool kWide>
+template <int kXBits, int kWBits, int kTerms, int kBlocks, int kCols, bool kWide>
 hipError_t launch_rows_shape(const LinearArgs &A, dim3 grid, hipStream_t stream)
 {
-    typedef RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols, kWide> S;
+    typedef RowsShape<kXBits, kWBits, kTerms, kBlocks, kCols, kWide> S;
     static LdsLimitOnce limit;
-    const hipError_t e = limit.set((const void *)linear_rows_kernel<kXBits, kWBits, kPlanes, kBlocks, kCols, kWide>, S::lds);
+    const hipError_t e = limit.set((const void *)linear_rows_kernel<kXBits, kWBits, kTerms, kBlocks, kCols, kWide>, S::lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((linear_rows_kernel<kXBits, kWBits, kPlanes, kBlocks, kCols, kWide>), grid, dim3(64 * S::waves), S::lds, stream, A);
+    hipLaunchKernelGGL((linear_rows_kernel<kXBits, kWBits, kTerms, kBlocks, kCols, kWide>), grid, dim3(64 * S::waves), S::lds, stream, A);
     return hipGetLastError();
 }
 
-template <int kXBits, int kWBits, int kPlanes, int kBlocks, int kCols>
+template <int kXBits, int kWBits, int kTerms, int kBlocks, int kCols>
 hipError_t launch_rows(const LinearArgs &A, hipStream_t stream)
 {
     // by expert: as many workgroups along the rows as an expert needs that has twice its share; they go on where it has more
@@ -205,29 +224,29 @@ hipError_t launch_rows(const LinearArgs &A, hipStream_t stream)
     // Two workgroups on a compute unit hide one another's first loads and last sums; one alone gets more loads in flight.  8-bit codes
     // of 16 tokens, K = 4096: 256 workgroups 7.4 us in pairs and 6.6 us alone, 688 of them 14.5 and 16.6 us.  Packed weights leave
     // room for deep rings either way (688 workgroups 9.9 and 12.6 us, 256 of them 4.6 and 4.8 us).
-    constexpr bool kPair = RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols, false>::exists;
+    constexpr bool kPair = RowsShape<kXBits, kWBits, kTerms, kBlocks, kCols, false>::exists;
     if constexpr (kPair) {
-        if (kWBits < 8 || (int64_t)grid.x * grid.y * grid.z > 256) return launch_rows_shape<kXBits, kWBits, kPlanes, kBlocks, kCols, false>(A, grid, stream);
+        if (kWBits < 8 || (int64_t)grid.x * grid.y * grid.z > 256) return launch_rows_shape<kXBits, kWBits, kTerms, kBlocks, kCols, false>(A, grid, stream);
     }
     if constexpr (!kPair || kWBits == 8) {
-        static_assert(RowsShape<kXBits, kWBits, kPlanes, kBlocks, kCols, true>::exists, "fits the LDS");
-        return launch_rows_shape<kXBits, kWBits, kPlanes, kBlocks, kCols, true>(A, grid, stream);
+        static_assert(RowsShape<kXBits, kWBits, kTerms, kBlocks, kCols, true>::exists, "fits the LDS");
+        return launch_rows_shape<kXBits, kWBits, kTerms, kBlocks, kCols, true>(A, grid, stream);
     }
 }
 
-// blocks x cols: 1x1, 1x2, 1x4, 2x1, 2x2, 4x2; of a gradient's planes 1x1, 1x2, 2x1 and (two planes) 2x2
-template <int kXBits, int kWBits, int kPlanes>
+// blocks x cols: 1x1, 1x2, 1x4, 2x1, 2x2, 4x2; of a gradient's terms 1x1, 1x2, 2x1 and (two terms) 2x2
+template <int kXBits, int kWBits, int kTerms>
 hipError_t launch_rows_of(const LinearArgs &A, int blocks, int cols, hipStream_t stream)
 {
-    if constexpr (kPlanes == 1) {
+    if constexpr (kTerms == 1) {
         if (blocks == 4) return launch_rows<kXBits, kWBits, 1, 4, 2>(A, stream);
         if (cols == 4) return launch_rows<kXBits, kWBits, 1, 1, 4>(A, stream);
     }
-    if constexpr (kPlanes < 3) {
-        if (blocks == 2 && cols == 2) return launch_rows<kXBits, kWBits, kPlanes, 2, 2>(A, stream);
+    if constexpr (kTerms < 3) {
+        if (blocks == 2 && cols == 2) return launch_rows<kXBits, kWBits, kTerms, 2, 2>(A, stream);
     }
-    if (blocks == 2) return launch_rows<kXBits, kWBits, kPlanes, 2, 1>(A, stream);
-    return cols == 2 ? launch_rows<kXBits, kWBits, kPlanes, 1, 2>(A, stream) : launch_rows<kXBits, kWBits, kPlanes, 1, 1>(A, stream);
+    if (blocks == 2) return launch_rows<kXBits, kWBits, kTerms, 2, 1>(A, stream);
+    return cols == 2 ? launch_rows<kXBits, kWBits, kTerms, 1, 2>(A, stream) : launch_rows<kXBits, kWBits, kTerms, 1, 1>(A, stream);
 }
 
 }  // namespace bq

@@ -12,7 +12,8 @@
 //
 // Bound by the matrix cores (60 .. 65 % busy) at the clock that the power limit leaves them, by what part of the last round of tiles is full,
 // and with packed codes by the vector instructions that unpack them, 2.7 per matrix instruction.  4-bit codes, 16384 tokens, 8192 -> 8192: 745 us, 2.95 POP/s, where a loop of the same instruction on random registers reaches 4.2; 8-bit codes,
-// 1777 tokens, 4096 -> 11008: 80 us, 2.0 POP/s; a gradient's two planes, 2048 tokens, 4096 -> 4096: 57.5 us, 2.4 POP/s.
+// 1777 tokens, 4096 -> 11008: 80 us, 2.0 POP/s; a gradient's two terms, 2048 tokens, 4096 -> 4096: 104 us, 1.3 PFLOP/s of binary16, where a loop
+// of the same instruction on random registers reaches 1.96.
 #pragma once
 
 #include <type_traits>
@@ -21,7 +22,7 @@
 
 namespace bq {
 
-// Waves of a workgroup along tokens and channels, 16-row pieces of a wave along tokens (of x's rows: planes count); 64 channels per wave.
+// Waves of a workgroup along tokens and channels, 16-row pieces of a wave along tokens (of x's rows: terms count); 64 channels per wave.
 // kLds: what the ring may take of a compute unit's LDS, in KB.
 template <int kWavesT, int kWavesN, int kPieces, int kLds>
 struct TileShape {
@@ -33,11 +34,11 @@ struct TileShape {
 
 constexpr int kMostStages = 4;
 
-// The ring: matrix instructions along a stage's codes (64 each), bytes of a stage's rows, stages that fit.
+// The ring: matrix instructions along a stage's codes (64 each, of a gradient's terms 32), bytes of a stage's rows, stages that fit.
 template <int kXBits, int kWBits, typename Shape>
 struct TileStages {
-    static constexpr int steps = 2;
-    static constexpr int x_row = steps * 8 * kXBits, w_row = steps * 8 * kWBits;
+    static constexpr int steps = 2, codes = steps * (kXBits == 16 ? 32 : 64);
+    static constexpr int x_row = codes * kXBits / 8, w_row = codes * kWBits / 8;
     static constexpr int bytes = Shape::x_rows * x_row + Shape::w_rows * w_row;
     static constexpr int fit = Shape::lds / bytes;
     static constexpr int depth = fit < kMostStages ? fit : kMostStages;
@@ -51,47 +52,39 @@ __device__ __forceinline__ int w_turn(int row)
 }
 
 // f for weights that lie across, rows of kRowBytes: a transposing read takes 8 bytes per lane, 32 lanes at a time, of 16 neighbouring
-// bytes of 8 rows (8 bits) or 8 of 16 rows (4 and 2 bits) from either of two places 32 rows apart.  (The latter read every bank twice;
+// bytes of 8 rows (8 bits) or 8 of 16 rows (4 and 2 bits) from either of two places 16 rows apart.  (The latter read every bank twice;
 // they move half as much.)
 template <int kRowBytes, int kBits>
 __device__ __forceinline__ int across_turn(int row)
 {
-    if (kBits == 8) return kRowBytes == 256 ? (row & 7) | ((row >> 2) & 8) : ((row >> 1) & 3) | ((row >> 3) & 4);
+    if (kBits == 8) return kRowBytes == 256 ? (row & 7) | ((row >> 1) & 8) : ((row >> 1) & 3) | ((row >> 2) & 4);
     return kRowBytes == 128 ? (row >> 1) & 7 : kRowBytes == 64 ? (row >> 2) & 3 : (row >> 3) & 1;
 }
 
-// 16 codes of 2 bits out of two words of pairs, the even channel's (odd = 0) or the odd one's, as bytes that hold 64 times the code; 0, 2,
-// 4, 6, 1, 3, 5, 7 of either word
-__device__ __forceinline__ i32x4 pair_codes(const uint32_t (&w)[2], int odd)
-{
-    i32x4 r;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        r[2 * j] = (int)((odd ? w[j] << 4 : w[j] << 6) & 0xC0C0C0C0u);
-        r[2 * j + 1] = (int)((odd ? w[j] : w[j] << 2) & 0xC0C0C0C0u);
-    }
-    return r;
-}
-
-// kAcross: the weights lie with the channels contiguous, [summed index][channel], and a stage is 128 rows of them; what a lane needs, 16
+// kTerms: 1 for codes of 8 or 4 bits; 2 or 3 for a gradient, whose x are binary16 terms (kXBits 16, bq_linear_bwd.hip) and whose sums are
+// float32, those of the first terms and those of the others apart.
+// kAcross: the weights lie with the channels contiguous, [summed index][channel], and a stage is 64 rows of them; what a lane needs, 16
 // codes of one channel, comes out of LDS by reads that transpose.  Piece j of the first operand is then channels 16 j .. 16 j + 15; of
 // 2-bit codes, which are read as fields of 4 bits, the even or (odd j) the odd ones of 32 (j / 2) .. 32 (j / 2) + 31.
-template <int kXBits, int kWBits, int kPlanes, typename Shape, bool kAcross = false>
+template <int kXBits, int kWBits, int kTerms, typename Shape, bool kAcross = false>
 __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearArgs A)
 {
     typedef TileStages<kXBits, kWBits, Shape> Stages;
     constexpr int kSteps = Stages::steps, kDepth = Stages::depth;
     constexpr int kXRow = Stages::x_row, kWRow = Stages::w_row;
-    constexpr int kXWords = kXRow / 16, kWWords = kWRow / 16;  // of a lane: 32 codes of every 16-row piece
+    constexpr bool kFloat = kXBits == 16;
+    static_assert(kFloat == (kTerms > 1) && (!kFloat || kAcross || kWBits == 8), "codes, or a gradient");
+    typedef typename SumType<kFloat>::type Sum;
+    constexpr int kXWords = kXRow / 16, kWWords = kWRow / 16 < 2 ? 2 : kWRow / 16;  // of a lane: a quarter of every row of 16
     constexpr int kWLine = kAcross ? Shape::w_rows * kWBits / 8 : kWRow;  // bytes of w's rows in LDS
-    static_assert(!kAcross || kXBits == 8, "digits");
+    static_assert(!kAcross || kFloat, "a gradient");
     constexpr int kXBytes = Shape::x_rows * kXRow, kWBytes = Shape::w_rows * kWRow, kStage = kXBytes + kWBytes;
     constexpr int kXLoads = kXBytes / 1024 / Shape::waves, kWCount = kWBytes / 1024, kWLoads = (kWCount + Shape::waves - 1) / Shape::waves;
     static_assert(kXLoads * 1024 * Shape::waves == kXBytes && (kWCount % Shape::waves == 0 || Shape::waves % kWCount == 0),
                   "whole loads per wave, or some waves load the same");
-    static_assert(Shape::pieces % kPlanes == 0 && (kPlanes == 1 || kXBits == 8), "planes of a token in one wave");
-    constexpr int kTokens = Shape::x_rows / kPlanes, kP = Shape::pieces;
-    constexpr bool kNatural = kXBits != kWBits && !kAcross;  // (digits are written in the order that they meet)
+    static_assert(Shape::pieces % kTerms == 0, "terms of a token in one wave");
+    constexpr int kTokens = Shape::x_rows / kTerms, kP = Shape::pieces;
+    constexpr bool kNatural = kXBits != kWBits;
     extern __shared__ __align__(16) uint8_t tile_lds[];
 
     // which tile: workgroups go round the 8 XCDs, each of which takes a contiguous eighth of the tiles; within it 8 tiles along the
@@ -121,8 +114,8 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
 #pragma unroll
     for (int i = 0; i < kXLoads; ++i) {
         const int q = i * Shape::waves + wave, row = q * (1024 / kXRow) + lane / (kXRow / 16);
-        const int plane = kPlanes == 1 ? 0 : (q * (1024 / kXRow) / 16) % kPlanes;
-        const int token = kPlanes == 1 ? row : (row / (16 * kPlanes)) * 16 + row % 16;
+        const int plane = kTerms == 1 ? 0 : (q * (1024 / kXRow) / 16) % kTerms;
+        const int token = kTerms == 1 ? row : (row / (16 * kTerms)) * 16 + row % 16;
         const int last = (int)(rt.row_end - rt.row0) - 1;
         x_piece[i] = (lane % (kXRow / 16)) ^ lds_turn<kXRow, kXWords / 4>(row);
         x_base[i] = A.x + plane * A.plane_step + rt.row0 * A.ldx;
@@ -143,7 +136,7 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
             w_off[i] = (uint32_t)(row < last ? row : last) * (uint32_t)A.ldw + w_piece[i] * 16;
         }
     }
-    const int stages = (A.k + 64 * kSteps - 1) / (64 * kSteps);
+    const int stages = (A.k + Stages::codes - 1) / Stages::codes;
     const int x_tail = (int)((int64_t)A.k * kXBits / 128) % (kXRow / 16), w_tail = (int)((int64_t)A.k * kWBits / 128) % (kWRow / 16);  // pieces of the last stage
     constexpr int kLoads = kXLoads + kWLoads;
     auto load = [&](int s, int place, int n) {  // the n-th of stage s's loads, into a place of the ring
@@ -152,10 +145,10 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
             const bool missing = x_tail && s == stages - 1 && x_piece[n] >= x_tail;  // a piece behind the last input: any other one
             load_to_lds(at + n * Shape::waves * 1024, missing ? x_off[n] - x_piece[n] * 16 : x_off[n], x_base[n] + (int64_t)s * kXRow);
         } else if constexpr (kAcross) {
-            // rows behind the last: the last one (the digits there are 0)
-            const int i = n - kXLoads, behind = s == stages - 1 ? s * 128 + w_piece[i] - (A.w_rows - 1) : 0;
+            // rows behind the last: the last one (the terms there are 0)
+            const int i = n - kXLoads, behind = s == stages - 1 ? s * Stages::codes + w_piece[i] - (A.w_rows - 1) : 0;
             load_to_lds(at + kXBytes + (i * Shape::waves + w_wave - wave) * 1024, w_off[i] - (behind > 0 ? behind * (uint32_t)A.ldw : 0u),
-                        w_base + (int64_t)s * 128 * A.ldw);
+                        w_base + (int64_t)s * Stages::codes * A.ldw);
         } else {
             const int i = n - kXLoads;
             const bool missing = w_tail && s == stages - 1 && w_piece[i] >= w_tail;
@@ -172,22 +165,21 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
         v[4 * h] = q.x; v[4 * h + 1] = q.y; v[4 * h + 2] = q.z; v[4 * h + 3] = q.w;
     };
     // (across: the address that a lane gives is another one's row)
-    const int across_row = 32 * g + (kWBits == 8 ? r16 >> 1 : r16);
+    const int across_row = 16 * g + (kWBits == 8 ? r16 >> 1 : r16);
     const int across_at = across_row * kWLine + ((wave_n * (kWBits / 2)) ^ across_turn<kWLine, kWBits>(across_row)) * 16 +
                           (kWBits == 8 ? r16 & 1 : 0) * 8;
     auto read_w = [&](int place, int n, int h, uint32_t (&v)[4][kWWords]) {
         const int j = n % 4;
         if constexpr (kAcross) {
-            const int rows = h * 16 + n / 4 * 8, half = kWBits == 8 ? 0 : j % 2 * 8, piece = kWBits == 8 ? j : kWBits == 4 ? j / 2 : 0;
-            const int at = place * kStage + kXBytes + (across_at ^ (piece * 16)) + half + rows * kWLine;
-            const int to = kWBits == 2 ? 2 * j + h : j, word = kWBits == 8 ? 4 * h + n / 4 * 2 : kWBits == 4 ? 2 * h : 0;
+            const int half = kWBits == 8 ? 0 : j % 2 * 8, piece = kWBits == 8 ? j : kWBits == 4 ? j / 2 : 0;
+            const int at = place * kStage + kXBytes + (across_at ^ (piece * 16)) + half + h * 8 * kWLine;
             typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
             i32x2 q;
             if constexpr (kWBits == 8)
                 q = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(tile_lds + at));
             else
                 q = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2 *)(tile_lds + at));
-            v[to][word] = (uint32_t)q[0]; v[to][word + 1] = (uint32_t)q[1];
+            v[j][2 * h] = (uint32_t)q[0]; v[j][2 * h + 1] = (uint32_t)q[1];
             return;
         }
         const uint8_t *p = tile_lds + place * kStage + kXBytes + (w_row + j * 4) * kWRow;
@@ -215,10 +207,11 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
     // the barrier the reads of 8 waves would hold up everyone's products.
     constexpr int kRing = kP == 2 ? 2 : kP % 4 == 0 ? 4 : 3, kX = kP == 2 ? 2 : 1;  // (two pieces are all read ahead: x alternates like w)
     static_assert(kP % kRing == 0, "the ring's places are the same in every stage");
-    constexpr int kWTurns = kAcross || kWWords == 8 ? 2 : 1, kWEach = !kAcross || kWBits == 4 ? 4 : kWBits;
+    constexpr int kWTurns = (kAcross && kWBits == 8) || kWWords == 8 ? 2 : 1, kWEach = kAcross && kWBits == 2 ? 2 : 4;
     constexpr int kXReads = kXWords / 4, kWReads = kWTurns * kWEach;  // of a piece of x; of all of w
     constexpr int kFirst = kWReads + 2 * kXReads;  // reads that a stage starts from
-    i32x4 acc[kP][4] = {};
+    constexpr int kSums = kFloat ? kP / kTerms * 2 : kP;
+    Sum acc[kSums][4] = {};
     uint32_t wv[2][4][kWWords], xv[kX][kRing][kXWords];  // (w's codes alternate: in one array every stage began by copying them)
     auto first_read = [&](int place, int n, uint32_t (&wv)[4][kWWords], uint32_t (&xv)[kRing][kXWords]) {
         // w's first halves, x's first piece, w's other halves, x's second piece
@@ -240,12 +233,14 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
         for (int h = 0; h < kSteps; ++h)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if constexpr (kAcross && kWBits == 2)
-                    a[h][j] = pair_codes(wv[j / 2 * 2 + h], j % 2);
+                if constexpr (kAcross)
+                    a[h][j] = kWBits == 8 ? half_codes8(wv[j][2 * h], wv[j][2 * h + 1]) : kWBits == 4 ? half_codes4(wv[j][h]) : half_codes2(wv[j / 2][h], j % 2);
+                else if constexpr (kFloat)
+                    a[h][j] = half_codes8(wv[j][2 * h], wv[j][2 * h + 1]);
                 else
                     a[h][j] = step_codes<kWBits, kNatural>(wv[j], h);
             }
-        i32x4 b = step_codes<kXBits, kNatural>(xv[0], 0);
+        i32x4 b = step_codes<kXBits == 16 ? 8 : kXBits, kNatural>(xv[0], 0);
 #pragma unroll
         for (int q = 0; q < kSteps * kP; ++q) {
             constexpr int kOver = 2 * kSteps, kTurn = kSteps * kP - kOver;  // from here on the reads belong to the next stage
@@ -269,9 +264,12 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
                 for (int n = (q - kTurn) * kFirst / kOver; n < (q - kTurn + 1) * kFirst / kOver; ++n) first_read(next_place, n, wn, xn);
             }
             i32x4 next = b;
-            if (q + 1 < kSteps * kP) next = step_codes<kXBits, kNatural>(xv[((q + 1) / kSteps) % kRing], (q + 1) % kSteps);
+            if (q + 1 < kSteps * kP) next = step_codes<kXBits == 16 ? 8 : kXBits, kNatural>(xv[((q + 1) / kSteps) % kRing], (q + 1) % kSteps);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[h][j], b, acc[i][j], 0, 0, 0);
+            for (int j = 0; j < 4; ++j) {
+                Sum &sum = acc[kFloat ? i / kTerms * 2 + (i % kTerms != 0) : i][j];
+                sum = multiply(a[h][j], b, sum);
+            }
             b = next;
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -320,21 +318,22 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
     stage(s, place, 0, wv[0], wv[1], xv[0], xv[kX - 1], std::integral_constant<int, 0>{});
 
     // (all loads in flight together: one after another, a token's scale at a time, they were a third of the time behind the last stage)
-    constexpr int kOut = kP / kPlanes;
+    constexpr int kOut = kP / kTerms;
     const int64_t t0 = rt.row0 + wave_t * kOut * 16 + r16;
     int64_t token[kOut];
-    float xs[kOut];
 #pragma unroll
     for (int i = 0; i < kOut; ++i) token[i] = t0 + 16 * i < rt.row_end ? t0 + 16 * i : rt.row_end - 1;
-    token_scales(A, token, xs);
-    if constexpr (kAcross) {  // a gradient has no scales and no bias of the channels
-        constexpr int kRun = kWBits == 2 ? 8 : 4, kRuns = 16 / kRun;  // neighbouring channels of a lane
+    if constexpr (kFloat) {  // a gradient has no scales and no bias of the channels
+        // neighbouring channels of a lane: 16, or as many as the pieces of weights that lie across leave together
+        constexpr int kRun = !kAcross ? 16 : kWBits == 2 ? 8 : 4, kRuns = 16 / kRun;
         const int o = o0 + wave_n * 64 + g * kRun;
+        int exponent[kOut];
+#pragma unroll
+        for (int i = 0; i < kOut; ++i) exponent[i] = ((const int *)A.xs)[token[i]];
 #pragma unroll
         for (int i = 0; i < kOut; ++i) {
             const int64_t t = t0 + 16 * i;
             if (t >= rt.row_end) continue;
-            const TokenScale s = token_scale<kPlanes>(xs[i], A.factor);
 #pragma unroll
             for (int j = 0; j < kRuns; ++j) {
                 const int first = o + 4 * kRun * j;
@@ -342,64 +341,58 @@ __global__ __launch_bounds__(Shape::threads, 2) void linear_tile_kernel(LinearAr
                 float v[kRun];
 #pragma unroll
                 for (int r = 0; r < kRun; ++r) {
-                    int part[kPlanes];
-#pragma unroll
-                    for (int p = 0; p < kPlanes; ++p)
-                        part[p] = kWBits == 2 ? acc[i * kPlanes + p][2 * j + r % 2][r / 2] : acc[i * kPlanes + p][j][r % 4];
-                    v[r] = scaled<kPlanes>(part, s);
+                    const int piece = kRun == 16 ? r / 4 : kRun == 8 ? 2 * j + r % 2 : j, at = kRun == 8 ? r / 2 : r % 4;
+                    v[r] = ldexpf(terms_sum(acc[2 * i][piece][at], acc[2 * i + 1][piece][at]) * A.factor, exponent[i]);
                 }
                 store_results<kRun>(A, t * A.ldy + first, v, A.n - first);
             }
         }
-        return;
-    }
-    const int o = o0 + wave_n * 64 + g * 16;
-    if (o >= A.n) return;
-    float ws[16], bias[16];
-    int64_t channel[16];
+    } else {
+        const int o = o0 + wave_n * 64 + g * 16;
+        if (o >= A.n) return;
+        float xs[kOut], ws[16], bias[16];
+        int64_t channel[16];
 #pragma unroll
-    for (int c = 0; c < 16; ++c) channel[c] = (int64_t)rt.expert * A.n + (o + c < A.n ? o + c : A.n - 1);
-    channel_scales(A, channel, ws);
-    channel_bias(A, channel, bias);
+        for (int c = 0; c < 16; ++c) channel[c] = (int64_t)rt.expert * A.n + (o + c < A.n ? o + c : A.n - 1);
+        load_scales(A.xs, A.xs_f16, token, xs);
+        load_scales(A.ws, A.ws_f16, channel, ws);
+        channel_bias(A, channel, bias);
 #pragma unroll
-    for (int i = 0; i < kOut; ++i) {
-        if (t0 + 16 * i >= rt.row_end) continue;
-        const TokenScale s = token_scale<kPlanes>(xs[i], A.factor);
-        float v[16];
+        for (int i = 0; i < kOut; ++i) {
+            if (t0 + 16 * i >= rt.row_end) continue;
+            float v[16];
 #pragma unroll
-        for (int c = 0; c < 16; ++c) {
-            int part[kPlanes];
+            for (int c = 0; c < 16; ++c) v[c] = scaled(acc[i][c >> 2][c & 3], A.factor, xs[i], ws[c]);
+            if (A.bias) {
 #pragma unroll
-            for (int p = 0; p < kPlanes; ++p) part[p] = acc[i * kPlanes + p][c >> 2][c & 3];
-            v[c] = scaled<kPlanes>(part, s);
-            if (A.ws) v[c] *= ws[c];
-            if (A.bias) v[c] += bias[c];
+                for (int c = 0; c < 16; ++c) v[c] += bias[c];
+            }
+            store_results<16>(A, (t0 + 16 * i) * A.ldy + o, v, A.n - o);
         }
-        store_results<16>(A, (t0 + 16 * i) * A.ldy + o, v, A.n - o);
     }
 }
 
-template <int kXBits, int kWBits, int kPlanes, typename Shape, bool kAcross = false>
+template <int kXBits, int kWBits, int kTerms, typename Shape, bool kAcross = false>
 hipError_t launch_tile(const LinearArgs &A, hipStream_t stream)
 {
     constexpr size_t kLds = (size_t)TileStages<kXBits, kWBits, Shape>::depth * TileStages<kXBits, kWBits, Shape>::bytes;
     static LdsLimitOnce limit;
-    const hipError_t e = limit.set((const void *)linear_tile_kernel<kXBits, kWBits, kPlanes, Shape, kAcross>, kLds);
+    const hipError_t e = limit.set((const void *)linear_tile_kernel<kXBits, kWBits, kTerms, Shape, kAcross>, kLds);
     if (e != hipSuccess) return e;
     const int64_t n_tiles = (A.n + Shape::w_rows - 1) / Shape::w_rows;
-    const int64_t all = row_tiles_bound(A, Shape::x_rows / kPlanes) * n_tiles;
-    hipLaunchKernelGGL((linear_tile_kernel<kXBits, kWBits, kPlanes, Shape, kAcross>), dim3((unsigned)((all + 7) / 8 * 8)), dim3(Shape::threads), kLds,
+    const int64_t all = row_tiles_bound(A, Shape::x_rows / kTerms) * n_tiles;
+    hipLaunchKernelGGL((linear_tile_kernel<kXBits, kWBits, kTerms, Shape, kAcross>), dim3((unsigned)((all + 7) / 8 * 8)), dim3(Shape::threads), kLds,
                        stream, A);
     return hipGetLastError();
 }
 
-// x rows (tokens times planes) x channels
+// x rows (tokens times terms) x channels
 typedef TileShape<2, 4, 8, 160> TileLarge;   // 256 x 256
 typedef TileShape<2, 4, 6, 160> TileTall;    // 192 x 256, for 8-bit codes
 typedef TileShape<2, 4, 4, 160> TileMiddle;  // 128 x 256
 typedef TileShape<2, 2, 4, 80> TileSmall;    // 128 x 128, two workgroups per compute unit
 typedef TileShape<4, 2, 2, 160> TileDeep;    // 128 x 128, one of them with eight waves and all of the LDS
-typedef TileShape<4, 2, 6, 160> TileLarge3;  // 384 x 128, for three planes
-typedef TileShape<4, 2, 3, 160> TileDeep3;   // 192 x 128 (by four waves 333 tokens of 4096 -> 5120 took 30.7 us instead of 28.5)
+typedef TileShape<4, 2, 6, 160> TileLarge3;  // 384 x 128, for three terms
+typedef TileShape<4, 2, 3, 160> TileDeep3;   // 192 x 128
 
 }  // namespace bq

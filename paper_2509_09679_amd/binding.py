@@ -485,6 +485,10 @@ def _check_offsets(who: str, d: bq_linear, offsets) -> None:
     _refuse_tensors(who, (("offsets", offsets, _torch_types(-2), d.experts + 1, True),))
 
 
+def _bytes(workspace) -> int:
+    return 0 if workspace is None else workspace.numel()
+
+
 def bq_linear_fwd(x, xscale, w, wscale, bias, y, desc: bq_linear, stream=None) -> None:
     """desc: make_linear(x, w, wscale, y, ...); bias may be None."""
     _check_fwd("bq_linear_fwd", desc, x, xscale, w, wscale, bias, y)
@@ -501,13 +505,13 @@ def bq_linear_grouped_fwd(x, xscale, w, wscale, bias, offsets, y, desc: bq_linea
 def bq_linear_bwd(dy, w, wscale, dx, workspace, desc: bq_linear, stream=None) -> None:
     """desc: make_linear_bwd(dy, w, wscale, dx, ...); workspace: uint8, at least bq_linear_bwd_workspace_bytes(desc)."""
     _check_bwd("bq_linear_bwd", desc, dy, w, wscale, dx, workspace)
-    _check((_CALLS or _calls()).linear_bwd(dy, w, wscale, dx, workspace, workspace.numel(), desc, _stream_ptr(stream)))
+    _check((_CALLS or _calls()).linear_bwd(dy, w, wscale, dx, workspace, _bytes(workspace), desc, _stream_ptr(stream)))
 
 
 def bq_linear_grouped_bwd(dy, w, wscale, offsets, dx, workspace, desc: bq_linear, stream=None) -> None:
     _check_bwd("bq_linear_grouped_bwd", desc, dy, w, wscale, dx, workspace)
     _check_offsets("bq_linear_grouped_bwd", desc, offsets)
-    _check((_CALLS or _calls()).linear_grouped_bwd(dy, w, wscale, offsets, dx, workspace, workspace.numel(), desc, _stream_ptr(stream)))
+    _check((_CALLS or _calls()).linear_grouped_bwd(dy, w, wscale, offsets, dx, workspace, _bytes(workspace), desc, _stream_ptr(stream)))
 
 
 def bq_probe_copy(src, dst, nbytes: int, stream=None) -> None:

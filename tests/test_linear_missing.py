@@ -1,0 +1,28 @@
+"""Calls of the quantised linear layers with something missing or of other dimensions are refused as the library's errors (no GPU: nothing
+is launched)."""
+import pytest
+import torch
+
+from paper_2509_09679_amd import binding as B
+
+
+@pytest.fixture(autouse=True)
+def _cpu_is_the_current_device(monkeypatch):
+    monkeypatch.setattr(B, "_here", lambda: -1)
+    monkeypatch.setattr(B, "_stream_ptr", lambda stream=None: 0)
+
+
+def _backward(**changed):
+    y, w, ws, dx = torch.zeros(7, 5), torch.zeros(5, 32, dtype=torch.int8), torch.zeros(5), torch.zeros(7, 32)
+    a = dict(dy=y, w=w, wscale=ws, dx=dx, workspace=torch.zeros(256, dtype=torch.uint8), desc=B.make_linear_bwd(y, w, ws, dx))
+    a.update(changed)
+    return a
+
+
+@pytest.mark.parametrize("name", ["dy", "w", "wscale", "dx", "workspace"])
+@pytest.mark.parametrize("grouped", [False, True])
+def test_backward_without_a_tensor(name, grouped):
+    more = dict(offsets=torch.zeros(2, dtype=torch.int32)) if grouped else {}
+    with pytest.raises(B.BqError) as e:
+        (B.bq_linear_grouped_bwd if grouped else B.bq_linear_bwd)(**_backward(**{name: None}, **more))
+    assert e.value.status == 1, str(e.value)

@@ -394,6 +394,8 @@ def _torch_types(code: int):
 def bq_rows_quant8(x, codes, scales, stream=None) -> None:
     """x: [rows, cols] of any row type, codes: int8 [rows, cols], both with a contiguous last dimension; scales: [rows], float32 or
     float16."""
+    _require(x is not None and codes is not None and scales is not None, 1, "bq_rows_quant8: x, codes or scales is None")
+    _require(x.dim() == codes.dim() == 2, 2, "bq_rows_quant8: x and codes must be [rows, cols]")
     shape, (ld_x, step_x), (ld_codes, step_codes) = x.shape, x.stride(), codes.stride()
     rows, cols = shape
     here, values = _here(), _ROW_TYPES or _row_types()

@@ -26,3 +26,19 @@ def test_backward_without_a_tensor(name, grouped):
     with pytest.raises(B.BqError) as e:
         (B.bq_linear_grouped_bwd if grouped else B.bq_linear_bwd)(**_backward(**{name: None}, **more))
     assert e.value.status == 1, str(e.value)
+
+
+@pytest.mark.parametrize("name", ["x", "codes", "scales"])
+def test_quantiser_without_a_tensor(name):
+    a = dict(x=torch.zeros(3, 8), codes=torch.zeros(3, 8, dtype=torch.int8), scales=torch.zeros(3))
+    a[name] = None
+    with pytest.raises(B.BqError) as e:
+        B.bq_rows_quant8(**a)
+    assert e.value.status == 1, str(e.value)
+
+
+@pytest.mark.parametrize("x,codes", [((8,), (8,)), ((2, 3, 8), (2, 3, 8)), ((3, 8), (24,)), ((3, 8), (1, 3, 8)), ((8,), (1, 8)), ((), ())])
+def test_quantiser_of_other_dimensions(x, codes):
+    with pytest.raises(B.BqError) as e:
+        B.bq_rows_quant8(torch.zeros(x), torch.zeros(codes, dtype=torch.int8), torch.zeros(6))
+    assert e.value.status == 2, str(e.value)

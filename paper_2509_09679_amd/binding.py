@@ -605,17 +605,17 @@ def _linear_descriptor(rows: int, inputs: int, w, wscale, values, xbits: int, wb
 def make_linear(x, w, wscale, y, xbits: int = 8, wbits: int = 8, inputs: int = 0) -> bq_linear:
     """Descriptor for bq_linear_fwd (w: [outputs, bytes of a row]) and bq_linear_grouped_fwd (w: [experts, outputs, bytes]).  x: codes,
     [rows, bytes]; y: [rows, outputs].  inputs: where the last byte of a row is not full."""
+    _require(x.dim() == y.dim() == 2 and y.shape[0] == x.shape[0], 2, f"x and y must have the same rows: {tuple(x.shape)}, {tuple(y.shape)}")
     inputs = inputs or x.shape[-1] * 8 // xbits
     d = _linear_descriptor(x.shape[0], inputs, w, wscale, y, xbits, wbits)
-    _require(x.dim() == y.dim() == 2 and y.shape[0] == d.rows, 2, f"x and y must have the same rows: {tuple(x.shape)}, {tuple(y.shape)}")
     d.ld_x, d.ld_y = _row_stride(x, (inputs * xbits + 7) // 8), _row_stride(y, d.outputs)
     return d
 
 
 def make_linear_bwd(dy, w, wscale, dx, wbits: int = 8) -> bq_linear:
     """Descriptor for bq_linear_bwd and bq_linear_grouped_bwd.  dy: [rows, outputs], dx: [rows, inputs], of one type."""
-    d = _linear_descriptor(dy.shape[0], dx.shape[-1], w, wscale, dy, 8, wbits)
-    _require(dy.dim() == dx.dim() == 2 and dx.shape[0] == d.rows and dx.dtype == dy.dtype, 2,
+    _require(dy.dim() == dx.dim() == 2 and dx.shape[0] == dy.shape[0] and dx.dtype == dy.dtype, 2,
              f"dy and dx must have the same rows and type: {tuple(dy.shape)}, {tuple(dx.shape)}")
+    d = _linear_descriptor(dy.shape[0], dx.shape[-1], w, wscale, dy, 8, wbits)
     d.ld_x, d.ld_y = _row_stride(dx, d.inputs), _row_stride(dy, d.outputs)
     return d

@@ -42,3 +42,16 @@ def test_quantiser_of_other_dimensions(x, codes):
     with pytest.raises(B.BqError) as e:
         B.bq_rows_quant8(torch.zeros(x), torch.zeros(codes, dtype=torch.int8), torch.zeros(6))
     assert e.value.status == 2, str(e.value)
+
+
+@pytest.mark.parametrize("shapes", [dict(x=(32,)), dict(x=(1, 7, 32)), dict(x=()), dict(y=(5,)), dict(y=(7, 5, 1)), dict(y=()), dict(w=(32,)), dict(w=(1, 1, 5, 32)), dict(w=())])
+def test_descriptors_of_other_dimensions(shapes):
+    s = dict(x=(7, 32), w=(5, 32), y=(7, 5), dx=(7, 32))
+    s.update(shapes)
+    if "x" in shapes:
+        s["dx"] = shapes["x"]
+    w, y = torch.zeros(s["w"], dtype=torch.int8), torch.zeros(s["y"])
+    for make in (lambda: B.make_linear(torch.zeros(s["x"], dtype=torch.int8), w, torch.zeros(5), y), lambda: B.make_linear_bwd(y, w, torch.zeros(5), torch.zeros(s["dx"]))):
+        with pytest.raises(B.BqError) as e:
+            make()
+        assert e.value.status == 2, str(e.value)

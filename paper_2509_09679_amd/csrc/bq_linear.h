@@ -145,7 +145,6 @@ __device__ __forceinline__ void store_row_value(void *p, int64_t at, int dtype, 
 
 // ---- launchers --------------------------------------------------------------------------------------------
 hipError_t launch_linear_any(const LinearArgs &A, int xbits, int wbits, hipStream_t stream);  // bq_linear_any.hip
-int64_t linear_any_blocks(const LinearArgs &A);
 // few rows: bq_linear_rows.h; blocks x cols: 16-token blocks and 16-channel columns of a workgroup
 hipError_t launch_linear_rows8(const LinearArgs &A, int wbits, int blocks, int cols, hipStream_t stream);
 hipError_t launch_linear_rows4(const LinearArgs &A, int wbits, int blocks, int cols, hipStream_t stream);

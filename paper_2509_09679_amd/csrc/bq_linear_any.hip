@@ -72,11 +72,10 @@ __global__ __launch_bounds__(256) void linear_any_kernel(LinearArgs A, int xbits
 
 }  // namespace
 
-int64_t linear_any_blocks(const LinearArgs &A) { return row_tiles_bound(A, kTile) * ((A.n + kTile - 1) / kTile); }
-
 hipError_t launch_linear_any(const LinearArgs &A, int xbits, int wbits, hipStream_t stream)
 {
-    hipLaunchKernelGGL(linear_any_kernel, dim3((unsigned)linear_any_blocks(A)), dim3(256), 0, stream, A, xbits, wbits);
+    const int64_t blocks = row_tiles_bound(A, kTile) * ((A.n + kTile - 1) / kTile);
+    hipLaunchKernelGGL(linear_any_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, A, xbits, wbits);
     return hipGetLastError();
 }
 

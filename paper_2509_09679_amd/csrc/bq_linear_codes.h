@@ -57,7 +57,8 @@ __device__ __forceinline__ i32x4 step_codes(const uint32_t (&w)[kWords], int s)
 }
 
 // One wave instruction: 16 bytes per lane from base + offset into LDS, in lane order.  The compiler does not see it: the reader waits
-// for vmcnt itself, and for its own reads before their place is loaded again.
+// for vmcnt itself, and for its own reads before their place is loaded again.  (m0 is reserved: the compiler sets it where it needs it, and
+// naming it as clobbered gives a warning and the same code.)
 __device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, const uint8_t *base)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2" : : "v"(offset), "s"(lds), "s"(base) : "memory");

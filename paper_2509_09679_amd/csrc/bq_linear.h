@@ -13,6 +13,7 @@
 #pragma once
 
 #include "bq_device.h"
+#include "bq_linear_choice.h"
 
 namespace bq {
 
@@ -31,6 +32,8 @@ struct LinearArgs {
     float factor;  // of the fields' positions
     int w_rows;    // of weights that lie across (bq_linear_tile.h): the summed index may be padded beyond it
 };
+
+inline LinearSize size_of(const LinearArgs &A) { return LinearSize{A.rows, A.k, A.n, A.experts, A.offsets != nullptr, A.w_rows}; }
 
 // Rows of one expert that a workgroup takes: [row0, row_end), at most the tile's.
 struct RowTile {
@@ -150,7 +153,6 @@ hipError_t launch_linear_rows8(const LinearArgs &A, int wbits, int blocks, int c
 hipError_t launch_linear_rows4(const LinearArgs &A, int wbits, int blocks, int cols, hipStream_t stream);
 hipError_t launch_linear_rows_terms(const LinearArgs &A, int terms, int blocks, int cols, hipStream_t stream);
 // many: bq_linear_tile.h
-enum LinearTile { kTileLarge, kTileTall, kTileMiddle, kTileSmall, kTileDeep };
 hipError_t launch_linear_tile8(const LinearArgs &A, int wbits, LinearTile tile, hipStream_t stream);
 hipError_t launch_linear_tile4(const LinearArgs &A, int wbits, LinearTile tile, hipStream_t stream);
 hipError_t launch_linear_tile_terms(const LinearArgs &A, int terms, LinearTile tile, hipStream_t stream);
@@ -159,7 +161,7 @@ hipError_t launch_linear_tile_across(const LinearArgs &A, int wbits, int terms, 
 hipError_t launch_linear(const LinearArgs &A, int xbits, int wbits, hipStream_t stream);
 hipError_t launch_linear_terms(const LinearArgs &A, int terms, hipStream_t stream);
 // the gradient's product with the weights as the layer has them, [summed index][channel]; is it quicker than transposing them first?
-bool linear_across_is_quicker(const LinearArgs &across, const LinearArgs &turned, int wbits, int terms);
+bool linear_across_is_quicker(const LinearArgs &across, int wbits, int terms);
 hipError_t launch_linear_across(const LinearArgs &A, int wbits, int terms, hipStream_t stream);
 
 }  // namespace bq

@@ -415,7 +415,7 @@ hipError_t launch_linear_bwd(const void *dy, int64_t ld_dy, const void *w, int w
     across.ldw = ldw;
     across.w_step = R.w_step;
     across.w_rows = n;
-    const bool as_they_are = linear_across_is_quicker(across, A, wbits, terms);
+    const bool as_they_are = linear_across_is_quicker(across, wbits, terms);
     const int turn = as_they_are ? 0 : wbits;
     D.spread = as_they_are && wbits < 8;
     const hipError_t e = dtype == BQ_F32   ? prepare<float, 3>(D, R, turn, stream)

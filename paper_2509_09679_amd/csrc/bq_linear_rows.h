@@ -13,23 +13,6 @@
 
 namespace bq {
 
-// kWide: all of a compute unit's LDS for one workgroup, else half of it.
-template <int kXBits, int kWBits, int kTerms, int kBlocks, int kCols, bool kWide>
-struct RowsShape {
-    static constexpr int frags = kBlocks * kTerms;
-    static constexpr int codes = kXBits == 16 ? 64 : kWBits == 2 ? 256 : 128;   // of a step
-    static constexpr int x_row = codes * kXBits / 8, w_row = codes * kWBits / 8;  // bytes of a step's rows: 64, 128, 256
-    static constexpr int x_bytes = frags * 16 * x_row, w_bytes = kCols * 16 * w_row, step = x_bytes + w_bytes;
-    static constexpr int room = (kWide ? 160 : 80) * 1024;
-    static constexpr int waves = 16 * step <= room ? 8 : 4;
-    static constexpr int per_simd = kWide ? 2 : waves / 2;  // waves that have to fit (four alone would get registers they have no use for)
-    static constexpr int fit = room / (waves * step), depth = fit < 4 ? fit : 4;
-    static constexpr int pairs = kBlocks * kCols, chunk = pairs < waves ? pairs : waves;  // pieces joined at a time
-    static constexpr int joined = waves * chunk * 1024;
-    static constexpr int lds = waves * depth * step > joined ? waves * depth * step : joined;
-    static constexpr bool exists = depth >= 2;  // one step is multiplied while another is loaded
-};
-
 template <int kXBits, int kWBits, int kTerms, int kBlocks, int kCols, bool kWide>
 __global__ __launch_bounds__((64 * RowsShape<kXBits, kWBits, kTerms, kBlocks, kCols, kWide>::waves),
                              (RowsShape<kXBits, kWBits, kTerms, kBlocks, kCols, kWide>::per_simd)) void linear_rows_kernel(LinearArgs A)
@@ -217,16 +200,11 @@ hipError_t launch_rows_shape(const LinearArgs &A, dim3 grid, hipStream_t stream)
 template <int kXBits, int kWBits, int kTerms, int kBlocks, int kCols>
 hipError_t launch_rows(const LinearArgs &A, hipStream_t stream)
 {
-    // by expert: as many workgroups along the rows as an expert needs that has twice its share; they go on where it has more
-    const int64_t rows = A.offsets ? (2 * A.rows + A.experts - 1) / A.experts : A.rows;
-    const int64_t passes = (rows + 16 * kBlocks - 1) / (16 * kBlocks);
-    const dim3 grid((unsigned)((A.n + 16 * kCols - 1) / (16 * kCols)), (unsigned)(passes < 1024 ? passes : 1024), (unsigned)A.experts);
-    // Two workgroups on a compute unit hide one another's first loads and last sums; one alone gets more loads in flight.  8-bit codes
-    // of 16 tokens, K = 4096: 256 workgroups 7.4 us in pairs and 6.6 us alone, 688 of them 14.5 and 16.6 us.  Packed weights leave
-    // room for deep rings either way (688 workgroups 9.9 and 12.6 us, 256 of them 4.6 and 4.8 us).
+    const RowsGrid g = rows_grid(size_of(A), kBlocks, kCols);
+    const dim3 grid((unsigned)g.along_channels, (unsigned)g.along_rows, (unsigned)g.experts);
     constexpr bool kPair = RowsShape<kXBits, kWBits, kTerms, kBlocks, kCols, false>::exists;
     if constexpr (kPair) {
-        if (kWBits < 8 || (int64_t)grid.x * grid.y * grid.z > 256) return launch_rows_shape<kXBits, kWBits, kTerms, kBlocks, kCols, false>(A, grid, stream);
+        if (kWBits < 8 || !rows_alone(g)) return launch_rows_shape<kXBits, kWBits, kTerms, kBlocks, kCols, false>(A, grid, stream);
     }
     if constexpr (!kPair || kWBits == 8) {
         static_assert(RowsShape<kXBits, kWBits, kTerms, kBlocks, kCols, true>::exists, "fits the LDS");

@@ -22,28 +22,6 @@
 
 namespace bq {
 
-// Waves of a workgroup along tokens and channels, 16-row pieces of a wave along tokens (of x's rows: terms count); 64 channels per wave.
-// kLds: what the ring may take of a compute unit's LDS, in KB.
-template <int kWavesT, int kWavesN, int kPieces, int kLds>
-struct TileShape {
-    static constexpr int lds = kLds * 1024;
-    static constexpr int waves_t = kWavesT, waves_n = kWavesN, pieces = kPieces;
-    static constexpr int waves = kWavesT * kWavesN, threads = 64 * waves;
-    static constexpr int x_rows = kWavesT * kPieces * 16, w_rows = kWavesN * 64;
-};
-
-constexpr int kMostStages = 4;
-
-// The ring: matrix instructions along a stage's codes (64 each, of a gradient's terms 32), bytes of a stage's rows, stages that fit.
-template <int kXBits, int kWBits, typename Shape>
-struct TileStages {
-    static constexpr int steps = 2, codes = steps * (kXBits == 16 ? 32 : 64);
-    static constexpr int x_row = codes * kXBits / 8, w_row = codes * kWBits / 8;
-    static constexpr int bytes = Shape::x_rows * x_row + Shape::w_rows * w_row;
-    static constexpr int fit = Shape::lds / bytes;
-    static constexpr int depth = fit < kMostStages ? fit : kMostStages;
-};
-
 // f of the header comment for w's rows, which are read as i -> 16 (i / 4) + i % 4; x's: lds_turn
 template <int kRowBytes>
 __device__ __forceinline__ int w_turn(int row)
@@ -385,14 +363,5 @@ hipError_t launch_tile(const LinearArgs &A, hipStream_t stream)
                        stream, A);
     return hipGetLastError();
 }
-
-// x rows (tokens times terms) x channels
-typedef TileShape<2, 4, 8, 160> TileLarge;   // 256 x 256
-typedef TileShape<2, 4, 6, 160> TileTall;    // 192 x 256, for 8-bit codes
-typedef TileShape<2, 4, 4, 160> TileMiddle;  // 128 x 256
-typedef TileShape<2, 2, 4, 80> TileSmall;    // 128 x 128, two workgroups per compute unit
-typedef TileShape<4, 2, 2, 160> TileDeep;    // 128 x 128, one of them with eight waves and all of the LDS
-typedef TileShape<4, 2, 6, 160> TileLarge3;  // 384 x 128, for three terms
-typedef TileShape<4, 2, 3, 160> TileDeep3;   // 192 x 128
 
 }  // namespace bq

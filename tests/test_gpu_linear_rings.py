@@ -38,9 +38,7 @@ def test_forward(T, N, K, experts, xbits, wbits):
     assert (y[:offsets[0]] == 3).all() and (y[offsets[-1]:] == 3).all()
 
 
-@pytest.mark.parametrize("T,N,K,experts,wbits,terms", R.GRADIENT_CASES)
-def test_gradient(T, N, K, experts, wbits, terms):
-    dtype = "f32" if terms == 3 else "f16" if T % 2 else "bf16"
+def _check_gradient(T, N, K, experts, wbits, dtype):
     gen, offsets, qw, w, ws = _layer(T, N, K, experts, wbits)
     dy = torch.randn((T, N), generator=gen, device=DEV).to(TORCH[dtype])
     dx = torch.full((T, K), 3.0, dtype=TORCH[dtype], device=DEV)
@@ -51,7 +49,7 @@ def test_gradient(T, N, K, experts, wbits, terms):
     else:
         B.bq_linear_bwd(dy, w, ws, dx, work, d)
     # a term: 2^-24 and 2^-22 or 2^-33 of itself, 2^-50 of the row's largest; the sum: a rounding per 32 terms, and 22 (test_gpu_linear_grad_range.py)
-    term = 2.0 ** -24 + (2.0 ** -33 if terms == 3 else 2.0 ** -22) + (N / 32 + 22) * 2.0 ** -23
+    term = 2.0 ** -24 + (2.0 ** -33 if dtype == "f32" else 2.0 ** -22) + (N / 32 + 22) * 2.0 ** -23
     scales = ws.view(-1, N).double()
     for e, (a, b) in enumerate(zip(offsets[:-1], offsets[1:])):
         if a == b:
@@ -61,3 +59,18 @@ def test_gradient(T, N, K, experts, wbits, terms):
         f32 = term * (v.abs() @ q) + 2.0 ** -50 * v.abs().amax(1, keepdim=True) * q.sum(0)
         _within(dx[a:b], want, f32 + (lu.half_step(dtype) * (want.abs() + f32) + lu.smallest(dtype) if dtype != "f32" else 1e-40))
     assert (dx[:offsets[0]] == 3).all() and (dx[offsets[-1]:] == 3).all()
+
+
+@pytest.mark.parametrize("T,N,K,experts,wbits,terms", R.GRADIENT_CASES)
+def test_gradient(T, N, K, experts, wbits, terms):
+    _check_gradient(T, N, K, experts, wbits, "f32" if terms == 3 else "f16" if T % 2 else "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("N", [2504, 4095, 5063, 8000, 16376, 16383, 16400])
+def test_gradients_of_wide_layers_on_weights_as_they_lie(N, dtype):
+    # rows of terms from one piece of a wave to the widest that stay in registers, and those that do not, beside no transposition
+    T, K = 1100, 4160
+    for experts, wbits in ((0, 8), (3, 4)):
+        assert R.gradient_choice(T, N, K, experts, wbits, 3 if dtype == "f32" else 2).kernel.across
+        _check_gradient(T, N, K, experts, wbits, dtype)

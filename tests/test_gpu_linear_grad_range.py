@@ -113,3 +113,18 @@ def test_rows_of_any_size(T, N, K, dtype):
     dy = rng.uniform(-1, 1, size=(T, N)) * np.exp2(np.linspace(-100, 100, T).round())[:, None]
     dx, dy, ws = _layer(q, dy, rng.uniform(0.5, 1.0, size=(1, N)), 8, dtype)
     _check(dx, dy, ws, q, dtype, [0, T], _roundings(N))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,K", SHAPES)
+def test_rows_of_subnormal_numbers(T, N, K, dtype):
+    # scales of 1 leave dy as it is: rows of float32's or bfloat16's smallest numbers have all their digits
+    rng = np.random.default_rng([T, N, K, 4])
+    q = lu.draw_codes(rng, (1, N, K), 4)
+    dy = np.rint(rng.uniform(-9, 9, size=(T, N))) * np.exp2(np.linspace(-149 if dtype == "f32" else -133, -125, T).round())[:, None]
+    dx, dy, ws = _layer(q, dy, np.ones((1, N)), 4, dtype)
+    v, w = dy * ws[0], q[0].astype(np.float64)
+    want, size = v @ w, np.abs(v) @ np.abs(w)
+    f32 = (_term(dtype) + _roundings(N) * 2.0 ** -23) * size + 2.0 ** -150  # (the result may be subnormal, too)
+    lu.check(dx, want, f32 + (lu.half_step(dtype) * (np.abs(want) + f32) + lu.smallest(dtype) if dtype != "f32" else 0.0), "rows")
+    assert (np.abs(dx) > 0).any()

@@ -84,13 +84,13 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ uint32_t f16_pair(f16x2 v) { return __builtin_bit_cast(uint32_t, v); }
 
-// the fields of kBits at bit kAt of both halves of w, whose top bits are turned round, as codes
+// the fields of kBits at bit kAt of both halves of w, as codes: one instruction picks them, turns their top bits round and sets the exponent
 template <int kBits, int kAt>
 __device__ __forceinline__ uint32_t half_fields(uint32_t w)
 {
-    constexpr uint32_t kMask = ((1u << kBits) - 1) << kAt;
+    constexpr uint32_t kMask = ((1u << kBits) - 1) << kAt, kTurn = 0x6400u | 1u << (kAt + kBits - 1);
     constexpr float kStep = 1.0f / (1 << kAt), kOffset = -(1024.0f * kStep + (1 << (kBits - 1)));
-    const f16x2 v = __builtin_bit_cast(f16x2, (w & (kMask << 16 | kMask)) | 0x64006400u);
+    const f16x2 v = __builtin_bit_cast(f16x2, __builtin_amdgcn_bitop3_b32(w, kMask << 16 | kMask, kTurn << 16 | kTurn, 0x6A));  // (w & mask) ^ turn
     return f16_pair(__builtin_elementwise_fma(v, f16x2{(_Float16)kStep, (_Float16)kStep}, f16x2{(_Float16)kOffset, (_Float16)kOffset}));
 }
 
@@ -109,16 +109,16 @@ __device__ __forceinline__ i32x4 half_codes8(uint32_t lo, uint32_t hi)
 // 8 codes of 4 bits, as 0, 4, 1, 5, 2, 6, 3, 7
 __device__ __forceinline__ i32x4 half_codes4(uint32_t w)
 {
-    const uint32_t u = w ^ 0x88888888u, v = u >> 8;
-    return i32x4{(int)half_fields<4, 0>(u), (int)half_fields<4, 4>(u), (int)half_fields<4, 0>(v), (int)half_fields<4, 4>(v)};
+    const uint32_t v = w >> 8;
+    return i32x4{(int)half_fields<4, 0>(w), (int)half_fields<4, 4>(w), (int)half_fields<4, 0>(v), (int)half_fields<4, 4>(v)};
 }
 
 // the same of the even channel (odd = 0) or the odd one of 8 fields of 4 bits that hold two codes of 2 bits each
 __device__ __forceinline__ i32x4 half_codes2(uint32_t w, int odd)
 {
-    const uint32_t u = w ^ 0xAAAAAAAAu, v = u >> 8;
-    if (odd) return i32x4{(int)half_fields<2, 2>(u), (int)half_fields<2, 6>(u), (int)half_fields<2, 2>(v), (int)half_fields<2, 6>(v)};
-    return i32x4{(int)half_fields<2, 0>(u), (int)half_fields<2, 4>(u), (int)half_fields<2, 0>(v), (int)half_fields<2, 4>(v)};
+    const uint32_t v = w >> 8;
+    if (odd) return i32x4{(int)half_fields<2, 2>(w), (int)half_fields<2, 6>(w), (int)half_fields<2, 2>(v), (int)half_fields<2, 6>(v)};
+    return i32x4{(int)half_fields<2, 0>(w), (int)half_fields<2, 4>(w), (int)half_fields<2, 0>(v), (int)half_fields<2, 4>(v)};
 }
 
 // ---- what products of codes (int32 sums) and gradients (binary16 terms, float32 sums) have in common

@@ -106,8 +106,9 @@ inline double pieces(const LinearSize &A, int rows)
 }
 
 // What a kernel takes, in us.  The constants below are fits to a sweep of all kernels (1 .. 8192 tokens, (K, N) from (1024, 2048) to
-// (11008, 4096), (8192, 8192) and (4096, 32000), codes of 8, 4 and 2 bits): what they choose is within 2 % of the best of the
-// sweep's kernels on average.  Measured, 8-bit codes 4096 -> 4096, us:
+// (11008, 4096), (8192, 8192) and (4096, 32000), codes of 8, 4 and 2 bits).  In another sweep, of (512, 1024), (320, 11008) and batches of 8 and
+// 32 experts too, what they choose takes 2 to 5 % more than the best on average where that takes more than 10 us, and at worst 20 to
+// 43 %.  Measured, 8-bit codes 4096 -> 4096, us:
 //   tokens          1    16    32    64   128   256   512  1024  2048  4096  8192
 //   1x1           5.9   6.5   8.5  12.6  20.5  35.7  67.9   115
 //   2x2           6.4   6.9   7.4   7.4  10.9  18.0  30.9  53.9
@@ -174,9 +175,9 @@ inline LinearChoice choose_codes(const LinearSize &A, int xbits, int wbits)
 }
 
 // Gradients: a fit of the same kind to a sweep of their kernels (1 .. 8192 tokens, (N, K) from (320, 11008) and (512, 1024) to (11008, 4096)
-// and (8192, 8192), two and three terms, weights of 8, 4 and 2 bits as they lie and transposed).  What it chooses is within 1 % of the sweep's
-// best on average; the worst is 19 % off it where that takes more than 10 us.  Measured, 8-bit weights as they lie (few rows:
-// transposed) 4096 -> 4096, us:
+// and (8192, 8192), two and three terms, weights of 8, 4 and 2 bits as they lie and transposed): what it chooses takes 0.2 to 2.3 % more than the
+// sweep's best on average where that takes more than 10 us, and at worst 17 %.  Measured, 8-bit weights as they lie (few rows: transposed) 4096 ->
+// 4096, us:
 //   two terms, tokens       8    32   128   256   512  1024  2048  4096  8192
 //   1x1                   7.4    13    34    61   112
 //   2x2                    11    14    21    35    62
@@ -208,7 +209,8 @@ inline double terms_tile_us(const LinearSize &A, int wbits, const TermsTile &t, 
     const auto &c = across ? t.across : t.turned;
     const double rounds = pieces(A, t.tokens) * std::ceil((double)A.n / t.channels) / t.at_once, whole = std::floor(rounds), part = rounds - whole;
     const double last = part == 0.0 ? 0.0 : part < 0.5 ? c.least : c.least + (1.0 - c.least) * (2.0 * part - 1.0);
-    const double us = (whole + last) * (c.fixed + c.stage * A.k / 64.0), weights = weights_us(A, wbits);
+    const double stage = across && wbits < 8 ? 0.92 * c.stage : c.stage;  // (fields of packed codes take fewer instructions)
+    const double us = (whole + last) * (c.fixed + stage * A.k / 64.0), weights = weights_us(A, wbits);
     return c.launch + (us > weights ? us : weights);
 }
 

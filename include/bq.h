@@ -265,8 +265,9 @@ bq_status bq_linear_fwd(const void *x, const void *xscale, const void *w, const 
  * for float32, whatever the row's other entries are; what lies below 2^-50 of the row's largest |dy * wscale| is lost.  Products
  * are exact and sums float32, in an order that the descriptor, whether the call is grouped, and w's alignment to 16 bytes fix.  A
  * row with an infinity or a NaN in dy * wscale gives NaN throughout.
- *   dy: [rows][ld_y], dx: [rows][ld_x], both of dtype; workspace: at least the queried size, 256-byte aligned, its contents
- *   on entry are ignored; calls that may run at once need one each.  dx must not overlap the inputs. */
+ *   dy: [rows][ld_y], dx: [rows][ld_x], both of dtype; workspace: at least the queried size (two or three 16-bit numbers per
+ *   entry of dy, N rounded up to 128, and a byte per weight), 256-byte aligned, its contents on entry are ignored; calls that
+ *   may run at once need one each.  dx must not overlap the inputs. */
 size_t bq_linear_bwd_workspace_bytes(const bq_linear *desc); /* 0 if the descriptor is invalid */
 bq_status bq_linear_bwd(const void *dy, const void *w, const void *wscale, void *dx, void *workspace,
                         size_t workspace_bytes, const bq_linear *desc, void *stream);

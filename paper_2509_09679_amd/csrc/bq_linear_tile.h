@@ -4,16 +4,17 @@
 //
 // LDS rows are the codes of a stage (128 bytes, 64 or 32 of packed codes), rows of x and of w after one another.  A direct load writes its 64
 // lanes' pieces in lane order, so the order of a row's 16-byte pieces is made by which piece a lane loads: piece ^ f(row), with f such
-// that the 8 lanes of a 16-byte read that go together fall on different banks.
+// that the lanes of a read that go together fall on different banks.  (All but the reads of packed weights that lie across: across_turn.)
 //
 // Where a stage feeds two matrix instructions, a lane's 16 codes of the two are neighbours (32 g + 16 s .. of lane group g, step s):
 // with packed codes one read then serves both.  Row i of the first operand's piece j is channel 16 (i / 4) + 4 j + i % 4 of the wave's 64:
 // a lane ends with 16 consecutive channels of one token.
 //
-// Bound by the matrix cores (60 .. 65 % busy) at the clock that the power limit leaves them, by what part of the last round of tiles is full,
-// and with packed codes by the vector instructions that unpack them, 2.7 per matrix instruction.  4-bit codes, 16384 tokens, 8192 -> 8192: 745 us, 2.95 POP/s, where a loop of the same instruction on random registers reaches 4.2; 8-bit codes,
-// 1777 tokens, 4096 -> 11008: 80 us, 2.0 POP/s; a gradient's two terms, 2048 tokens, 4096 -> 4096: 104 us, 1.3 PFLOP/s of binary16, where a loop
-// of the same instruction on random registers reaches 1.96.
+// Bound by the matrix cores (60 .. 66 % busy where the rounds of tiles are full, 47 .. 55 % where the last one is not or tiles are small) at the
+// clock that the power limit leaves them, by what part of the last round is full, and with packed codes by the vector instructions that unpack
+// them, 2.6 per matrix instruction.  4-bit codes, 16384 tokens, 8192 -> 8192: 735 .. 770 us, 2.9 POP/s, where a loop of the same instruction on
+// random registers reaches 4.2; 8-bit codes, 1777 tokens, 4096 -> 11008: 80 .. 84 us, 2.0 POP/s; a gradient's two terms, 2048 tokens, 4096 -> 4096:
+// 104 .. 115 us, 1.2 .. 1.3 PFLOP/s of binary16, where a loop of the same instruction on random registers reaches 1.96.
 #pragma once
 
 #include <type_traits>
@@ -30,8 +31,8 @@ __device__ __forceinline__ int w_turn(int row)
 }
 
 // f for weights that lie across, rows of kRowBytes: a transposing read takes 8 bytes per lane, 32 lanes at a time, of 16 neighbouring
-// bytes of 8 rows (8 bits) or 8 of 16 rows (4 and 2 bits) from either of two places 16 rows apart.  (The latter read every bank twice;
-// they move half as much.)
+// bytes of 8 rows (8 bits) or 8 of 16 rows (4 and 2 bits) from either of two places 16 rows apart.  (The latter read every bank twice, a
+// fifth of LDS's busy cycles; they move half as much.)
 template <int kRowBytes, int kBits>
 __device__ __forceinline__ int across_turn(int row)
 {

@@ -606,6 +606,7 @@ def make_linear(x, w, wscale, y, xbits: int = 8, wbits: int = 8, inputs: int = 0
     """Descriptor for bq_linear_fwd (w: [outputs, bytes of a row]) and bq_linear_grouped_fwd (w: [experts, outputs, bytes]).  x: codes,
     [rows, bytes]; y: [rows, outputs].  inputs: where the last byte of a row is not full."""
     _require(x.dim() == y.dim() == 2 and y.shape[0] == x.shape[0], 2, f"x and y must have the same rows: {tuple(x.shape)}, {tuple(y.shape)}")
+    _require(xbits > 0, 6, f"make_linear: xbits={xbits}")
     inputs = inputs or x.shape[-1] * 8 // xbits
     d = _linear_descriptor(x.shape[0], inputs, w, wscale, y, xbits, wbits)
     d.ld_x, d.ld_y = _row_stride(x, (inputs * xbits + 7) // 8), _row_stride(y, d.outputs)

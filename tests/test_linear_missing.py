@@ -55,3 +55,11 @@ def test_descriptors_of_other_dimensions(shapes):
         with pytest.raises(B.BqError) as e:
             make()
         assert e.value.status == 2, str(e.value)
+
+
+@pytest.mark.parametrize("xbits", [0, -8, 3, 16])
+def test_descriptors_of_other_bits(xbits):
+    # no activation's bits: refused when the descriptor is made or by the call, never as another exception
+    x, w, ws, y = torch.zeros(7, 32, dtype=torch.int8), torch.zeros(5, 32, dtype=torch.int8), torch.zeros(5), torch.zeros(7, 5)
+    with pytest.raises(B.BqError):
+        B.bq_linear_fwd(x, torch.zeros(7), w, ws, None, y, B.make_linear(x, w, ws, y, xbits=xbits))
